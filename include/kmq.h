@@ -393,6 +393,115 @@ km_status kmeans_fit_hier(const km_points *P, int32_t k, const km_hier_params *h
 km_status kmeans_cost(const float *X, int64_t n, int32_t d, int64_t ldx, const float *C, int32_t k,
                       const int32_t *assign, double *out, km_stream stream);
 
+/* ---- Key/value cache in 8 bits ----------------------------------------------------------------------------------
+ *
+ * Keys and values of a transformer's past tokens as 8-bit codes in pages (blocks of `page` tokens), one scale per
+ * page and head, and the attention that reads them.  A sequence's position p is token p % page of page
+ * table[p / page].
+ */
+typedef enum {
+  KM_KV_I8 = 0, /* whole numbers -127 .. 127 */
+  KM_KV_F8 = 1  /* e4m3 (OCP, no infinities, largest 448) */
+} km_kv_format;
+
+typedef enum { KM_T_F32 = 0, KM_T_BF16 = 1, KM_T_F16 = 2 } km_type; /* rows given to and taken from the cache */
+
+/*
+ * The cache.  value = code * scale.
+ *   page: 16, 32, 64 or 128 tokens.  d: 16 .. 256, d % 16 == 0.  1 <= pages < 2^31.  heads * page * d < 2^31.
+ *   k: codes [pages][heads][page][d]; v: codes [pages][heads][d][page] (dims first: the attention sums over
+ *   tokens).  k_scale, v_scale: float[pages][heads].  k and v 16-byte aligned.  A new cache needs no contents.
+ */
+typedef struct km_kv_cache {
+  int32_t fmt; /* km_kv_format */
+  int32_t page;
+  int32_t heads;
+  int32_t d;
+  int64_t pages;
+  void *k;
+  void *v;
+  float *k_scale;
+  float *v_scale;
+} km_kv_cache;
+
+/*
+ * The sequences of a call.  Rows of a call (keys and values, queries, results) are packed over the sequences; those of
+ * sequence b are the LAST positions of it, up to position lens[b] - 1.
+ *   table: int32[n][table_ld], pages of each sequence, table_ld >= max_pages >= 1.  lens: int32[n], tokens of each
+ *   sequence, the call's own included.  starts: int32[n + 1], rows starts[b] .. starts[b + 1] - 1 are sequence b's;
+ *   NULL: every sequence has max_rows rows and rows = n * max_rows.  rows: rows of all sequences.  max_rows: the most
+ *   rows that one of them has.  max_len (0: not known): the longest of lens; it chooses launch shapes and no results.
+ * table, lens and starts are read on the device and checked there: a sequence whose length is outside
+ * [0, max_pages * page] or whose rows are not within [0, rows) or more than max_rows takes no part in the call (its rows are
+ * left as they are), and an entry of table outside [0, pages) that a position needs is a page that is not there.
+ */
+typedef struct km_kv_seqs {
+  int32_t n;
+  int32_t max_pages;
+  const int32_t *table;
+  int64_t table_ld;
+  const int32_t *lens;
+  const int32_t *starts;
+  int64_t rows;
+  int32_t max_rows;
+  int32_t max_len;
+} km_kv_seqs;
+
+/* Rows [row][head][dim] of a km_type: element strides of a row and a head; the dims are contiguous.  p 16-byte aligned,
+ * both strides multiples of 16 bytes. */
+typedef struct km_kv_rows {
+  void *p;
+  int64_t row;
+  int64_t head;
+} km_kv_rows;
+
+/*
+ * kv_write -- put the rows' keys and values into the cache.  For each page and head, and keys and values apart:
+ *   a = the largest finite |x| of the rows written there (an infinity counts as +-a, NaN as 0);
+ *   mul = qmax / a (fp32, 2^100 at most) without what lies below its eight leading bits; qmax = 127 (I8), 448 (F8);
+ *   where the page holds earlier tokens of the sequence and mul is larger than the page's, the page's; where it is smaller,
+ *   their codes become the code nearest to code * mul / (the page's mul);
+ *   code = the nearest to x * mul, ties to the even one; scale = 1 / mul in fp32.
+ * A 16-bit x times mul is exact in fp32, and fp32 rows are rounded as the exact product is, so codes do not depend on how
+ * the product is computed.  A call that writes a page's first token gives it a new scale.  Rows that fall before position 0
+ * or on a page that is not there are skipped.  No two sequences of a call may write the same page.
+ */
+km_status kv_write(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *k, const km_kv_rows *v,
+                   int32_t type, km_stream stream);
+
+/*
+ * kv_read -- the rows' keys and values from the cache: code * scale in fp32, rounded to the type (past its largest finite
+ * value, that value).  Rows before position 0 or on a page that is not there are zeros.
+ */
+km_status kv_read(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *k, const km_kv_rows *v,
+                  int32_t type, km_stream stream);
+
+/* kv_attend() flags */
+#define KM_KV_CAUSAL 1 /* a row at position p sees positions up to p; without it the whole sequence */
+
+/*
+ * kv_attend -- attention of the rows' queries over the cache: for query head hq of a row,
+ *   out = sum_j p_j v_j, p = softmax_j(scale <q, k_j>), keys and values of cache head hq / (q_heads / heads), over the
+ *   positions j of the sequence that the row sees: j <= its own with KM_KV_CAUSAL, and with window > 0 (then
+ *   KM_KV_CAUSAL is needed) the last `window` of these.  Positions on pages that are not there are not seen.
+ *   q, out: rows of q_heads heads of the type; lse (nullable): float[rows][q_heads], log sum_j exp(scale <q, k_j>).
+ *   A row that sees no position gets zeros and -infinity.
+ *   q_heads: a multiple of heads; max_rows * q_heads / heads < 2^30.  scale: finite, > 0.
+ *   ws (nullable): kv_attend_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the
+ *   pool.  Codes of positions inside a sequence have to be finite (kv_write makes no others); what lies behind its
+ *   end is not looked at.
+ *   fp32 queries: products and weights in two halves each (about 22 bits); 16-bit ones: their own bits, weights rounded to
+ *   fp16; sums, maxima and normalisation in fp32.
+ *   The result does not depend on scheduling.
+ */
+km_status kv_attend(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *q, int32_t q_heads, float scale,
+                    int32_t flags, int32_t window, const km_kv_rows *out, int32_t type, float *lse, void *ws,
+                    int64_t ws_bytes, km_stream stream);
+
+/* Bytes of ws that kv_attend uses for these arguments (0: none; < 0: a km_status). */
+int64_t kv_attend_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t q_heads, int32_t flags,
+                        int32_t window, int32_t type);
+
 /* Thread-local message for the last non-OK status ("" if none). */
 const char *km_last_error(void);
 

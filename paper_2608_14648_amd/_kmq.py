@@ -25,7 +25,7 @@ STATUS = {0: "KM_OK", -1: "KM_EINVAL", -2: "KM_EUNSUPPORTED", -3: "KM_ENOMEM", -
 EXPORTS = ("quantize", "rabitq_encode", "pca_fit_cov", "pca_project", "kmeans_assign", "kmeans_assign_noalloc",
            "kmeans_update",
            "kmeans_fit", "kmeans_fine", "kmeans_fit_hier", "kmeans_assign_pruned", "kmeans_fit_pruned", "kmeans_cost",
-           "km_last_error", "km_release")
+           "kv_write", "kv_read", "kv_attend", "kv_attend_bytes", "km_last_error", "km_release")
 
 
 class KmqError(RuntimeError):
@@ -58,6 +58,22 @@ class KmHierParams(ct.Structure):
                 ("iters_refine", ct.c_int32), ("flags", ct.c_int32)]
 
 
+class KmKvCache(ct.Structure):
+    _fields_ = [("fmt", ct.c_int32), ("page", ct.c_int32), ("heads", ct.c_int32), ("d", ct.c_int32),
+                ("pages", ct.c_int64), ("k", ct.c_void_p), ("v", ct.c_void_p), ("k_scale", ct.c_void_p),
+                ("v_scale", ct.c_void_p)]
+
+
+class KmKvSeqs(ct.Structure):
+    _fields_ = [("n", ct.c_int32), ("max_pages", ct.c_int32), ("table", ct.c_void_p), ("table_ld", ct.c_int64),
+                ("lens", ct.c_void_p), ("starts", ct.c_void_p), ("rows", ct.c_int64), ("max_rows", ct.c_int32),
+                ("max_len", ct.c_int32)]
+
+
+class KmKvRows(ct.Structure):
+    _fields_ = [("p", ct.c_void_p), ("row", ct.c_int64), ("head", ct.c_int64)]
+
+
 _lib = None
 
 
@@ -86,12 +102,17 @@ def lib():
             "kmeans_fit_pruned": [ct.POINTER(KmPoints), i32, i32, vp, vp, vp, vp, i32, ct.POINTER(KmPrune),
                                   ct.POINTER(KmFitStats), vp, vp],
             "kmeans_cost": [vp, i64, i32, i64, vp, i32, vp, vp, vp],
+            "kv_write": [vp, vp, vp, vp, i32, vp],
+            "kv_read": [vp, vp, vp, vp, i32, vp],
+            "kv_attend": [vp, vp, vp, i32, ct.c_float, i32, i32, vp, i32, vp, vp, i64, vp],
+            "kv_attend_bytes": [vp, vp, i32, i32, i32, i32],
             "km_release": [],
         }
         for name, args in sig.items():
             f = getattr(L, name)
             f.argtypes = args
             f.restype = ct.c_int
+        L.kv_attend_bytes.restype = i64
         L.km_last_error.argtypes = []
         L.km_last_error.restype = ct.c_char_p
         _lib = L

@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "common.hpp"
+#include "kv.hpp"
 
 namespace kmq {
 
@@ -1142,6 +1143,162 @@ km_status kmeans_cost(const float *X, int64_t n, int32_t d, int64_t ldx, const f
   km_status st = ws.alloc(sizeof(double) * 1024);
   if (st != KM_OK) return st;
   return launch_cost(X, n, d, ldx, C, k, assign, out, reinterpret_cast<double *>(ws.get()), s);
+}
+
+}  // extern "C"
+
+// ---- key/value cache -------------------------------------------------------------------------------------------------
+
+namespace kmq {
+
+static km_status check_cache(const km_kv_cache *c, KvCache *o) {
+  KMQ_CHECK(c != nullptr, KM_EINVAL, "cache descriptor is NULL");
+  KMQ_CHECK(c->fmt == KM_KV_I8 || c->fmt == KM_KV_F8, KM_EUNSUPPORTED, "unknown cache format %d", c->fmt);
+  KMQ_CHECK(c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128, KM_EINVAL,
+            "page = %d must be 16, 32, 64 or 128", c->page);
+  KMQ_CHECK(c->d >= 16 && c->d <= 256 && c->d % 16 == 0, KM_EINVAL, "d = %d must be a multiple of 16 up to 256", c->d);
+  KMQ_CHECK(c->heads >= 1 && (int64_t)c->heads * c->page * c->d < INT32_MAX, KM_EINVAL,
+            "heads = %d must be >= 1 and heads * page * d < 2^31", c->heads);
+  KMQ_CHECK(c->pages >= 1 && c->pages < (int64_t)INT32_MAX, KM_EINVAL, "pages = %lld outside [1, 2^31)",
+            (long long)c->pages);
+  KMQ_CHECK(c->k && c->v && c->k_scale && c->v_scale, KM_EINVAL, "NULL argument");
+  KMQ_CHECK(aligned16(c->k) && aligned16(c->v), KM_EINVAL, "codes must be 16-byte aligned");
+  const int shift = c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
+  *o = KvCache{c->fmt,   c->page, shift,      c->heads, c->d, c->pages, static_cast<uint8_t *>(c->k),
+               static_cast<uint8_t *>(c->v), c->k_scale, c->v_scale};
+  return KM_OK;
+}
+
+// OK with o->n == 0: a call without rows
+static km_status check_seqs(const km_kv_seqs *s, const KvCache &c, KvSeqs *o) {
+  KMQ_CHECK(s != nullptr, KM_EINVAL, "sequences descriptor is NULL");
+  KMQ_CHECK(s->n >= 0 && s->rows >= 0 && s->max_rows >= 0 && s->max_len >= 0, KM_EINVAL,
+            "n, rows, max_rows and max_len must be >= 0");
+  *o = KvSeqs{};
+  if (s->n == 0 || s->rows == 0 || s->max_rows == 0) return KM_OK;
+  KMQ_CHECK(s->table != nullptr && s->lens != nullptr, KM_EINVAL, "NULL argument");
+  KMQ_CHECK(s->max_pages >= 1 && s->table_ld >= s->max_pages, KM_EINVAL, "need table_ld >= max_pages >= 1");
+  KMQ_CHECK((int64_t)s->max_pages * c.page < (int64_t)INT32_MAX, KM_EINVAL, "max_pages * page = %lld outside [1, 2^31)",
+            (long long)s->max_pages * c.page);
+  KMQ_CHECK(s->starts != nullptr || s->rows == (int64_t)s->n * s->max_rows, KM_EINVAL,
+            "without starts rows must be n * max_rows");
+  KMQ_CHECK(s->rows < (int64_t)INT32_MAX && s->max_rows < (1 << 30), KM_EINVAL,
+            "rows = %lld outside [0, 2^31) or max_rows = %d outside [0, 2^30)", (long long)s->rows, s->max_rows);
+  const int cap = s->max_pages * c.page;
+  *o = KvSeqs{s->n,    s->max_pages, s->table,    s->table_ld,
+              s->lens, s->starts,    s->max_rows, s->max_len ? std::min(s->max_len, cap) : cap,
+              s->rows};
+  return KM_OK;
+}
+
+static km_status check_rows(const km_kv_rows *r, int32_t type, const char *name, KvRows *o) {
+  KMQ_CHECK(type == KM_T_F32 || type == KM_T_BF16 || type == KM_T_F16, KM_EUNSUPPORTED, "unknown type %d of rows", type);
+  const int unit = type == KM_T_F32 ? 4 : 8;
+  KMQ_CHECK(r != nullptr && r->p != nullptr, KM_EINVAL, "%s is NULL", name);
+  KMQ_CHECK(aligned16(r->p) && r->row % unit == 0 && r->head % unit == 0 && r->row >= 0 && r->head >= 0, KM_EINVAL,
+            "%s needs 16-byte alignment and row and head strides that are multiples of 16 bytes", name);
+  *o = KvRows{r->p, r->row, r->head};
+  return KM_OK;
+}
+
+static km_status check_grid(int64_t blocks) {
+  KMQ_CHECK(blocks < (int64_t)INT32_MAX, KM_EINVAL, "%lld workgroups: n, heads or max_rows too large", (long long)blocks);
+  return KM_OK;
+}
+
+static km_status kv_move(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *k, const km_kv_rows *v,
+                         int32_t type, bool write, km_stream stream) {
+  KvCache c;
+  KvSeqs s;
+  KvRows kr, vr;
+  km_status st = check_cache(cache, &c);
+  if (st == KM_OK) st = check_seqs(seqs, c, &s);
+  if (st != KM_OK || s.n == 0) return st;
+  st = check_rows(k, type, "k", &kr);
+  if (st == KM_OK) st = check_rows(v, type, "v", &vr);
+  if (st == KM_OK) st = check_grid(kv_move_blocks(c, s));
+  if (st != KM_OK) return st;
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  return write ? launch_kv_write(c, s, kr, vr, type, hs) : launch_kv_read(c, s, kr, vr, type, hs);
+}
+
+static km_status check_attend(const KvCache &c, const KvSeqs &s, int32_t q_heads, int32_t flags, int32_t window,
+                              int32_t type, KvAttend *o) {
+  KMQ_CHECK(type == KM_T_F32 || type == KM_T_BF16 || type == KM_T_F16, KM_EUNSUPPORTED, "unknown type %d of rows", type);
+  KMQ_CHECK(q_heads >= 1 && q_heads % c.heads == 0, KM_EINVAL, "q_heads = %d must be a multiple of heads = %d", q_heads,
+            c.heads);
+  KMQ_CHECK((flags & ~KM_KV_CAUSAL) == 0, KM_EINVAL, "unknown flags 0x%x", flags);
+  KMQ_CHECK(window >= 0 && (window == 0 || (flags & KM_KV_CAUSAL)), KM_EINVAL,
+            "window = %d must be >= 0, and > 0 only with KM_KV_CAUSAL", window);
+  *o = KvAttend{};
+  o->type = type;
+  o->group = q_heads / c.heads;
+  o->causal = flags & KM_KV_CAUSAL;
+  o->window = window;
+  KMQ_CHECK((int64_t)s.max_rows * o->group < (1 << 30), KM_EINVAL, "max_rows * q_heads / heads = %lld must be < 2^30",
+            (long long)s.max_rows * o->group);
+  return s.n ? check_grid(kv_attend_blocks(c, s, *o)) : KM_OK;
+}
+
+}  // namespace kmq
+
+extern "C" {
+
+km_status kv_write(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *k, const km_kv_rows *v,
+                   int32_t type, km_stream stream) {
+  g_err[0] = 0;
+  return kv_move(cache, seqs, k, v, type, true, stream);
+}
+
+km_status kv_read(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *k, const km_kv_rows *v,
+                  int32_t type, km_stream stream) {
+  g_err[0] = 0;
+  return kv_move(cache, seqs, k, v, type, false, stream);
+}
+
+int64_t kv_attend_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t q_heads, int32_t flags,
+                        int32_t window, int32_t type) {
+  g_err[0] = 0;
+  KvCache c;
+  KvSeqs s;
+  KvAttend a;
+  km_status st = check_cache(cache, &c);
+  if (st == KM_OK) st = check_seqs(seqs, c, &s);
+  if (st == KM_OK) st = check_attend(c, s, q_heads, flags, window, type, &a);
+  if (st != KM_OK) return st;
+  return s.n ? (int64_t)kv_attend_scratch(c, s, a) : 0;
+}
+
+km_status kv_attend(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *q, int32_t q_heads, float scale,
+                    int32_t flags, int32_t window, const km_kv_rows *out, int32_t type, float *lse, void *ws,
+                    int64_t ws_bytes, km_stream stream) {
+  g_err[0] = 0;
+  KvCache c;
+  KvSeqs s;
+  KvAttend a;
+  km_status st = check_cache(cache, &c);
+  if (st == KM_OK) st = check_seqs(seqs, c, &s);
+  if (st == KM_OK) st = check_attend(c, s, q_heads, flags, window, type, &a);
+  if (st != KM_OK) return st;
+  KMQ_CHECK(scale > 0.0f && std::isfinite(scale), KM_EINVAL, "scale = %g must be finite and > 0", (double)scale);
+  if (s.n == 0) return KM_OK;
+  st = check_rows(q, type, "q", &a.q);
+  if (st == KM_OK) st = check_rows(out, type, "out", &a.out);
+  if (st != KM_OK) return st;
+  a.scale = scale;
+  a.lse = lse;
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const int64_t need = (int64_t)kv_attend_scratch(c, s, a);
+  Scratch own(hs);
+  if (need && ws == nullptr) {
+    st = own.alloc((size_t)need);
+    if (st != KM_OK) return st;
+    ws = own.get();
+  } else if (need) {
+    KMQ_CHECK(ws_bytes >= need && aligned16(ws), KM_EINVAL, "ws needs %lld bytes (got %lld) and 16-byte alignment",
+              (long long)need, (long long)ws_bytes);
+  }
+  return launch_kv_attend(c, s, a, ws, hs);
 }
 
 }  // extern "C"

@@ -1,0 +1,459 @@
+"""The 8-bit key/value cache and the attention over it against the 64-bit oracle (oracle/kv.py).
+
+What is held in 8 bits is compared exactly: codes (as the values they stand for), scales and the rows read back.
+Attention is compared within a bound made of its roundings, per element:
+
+* the output's own rounding, u_out |o|;
+* the weights' rounding, u_w sum p |v| (fp16 for 16-bit rows, two halves for fp32 ones);
+* a weight's steps below fp16's normal range: 2^-40 of the largest weight times the largest value of its page, N of them;
+* the error of a weight's exponent, e = 2^-24 (d A + 4 T + 8) with A = the largest scale * sum |q||k| of the row (a dot
+  product of d terms in fp32) and T = the size of the exponents in base 2, and of sums of N terms, N 2^-24; numerator and
+  denominator each carry both: 2 (e + N 2^-24) sum p |v|.
+
+The log-sum-exp: e + (N + 4 |lse|) 2^-24.
+"""
+import math
+
+import numpy as np
+import pytest
+
+from gpu_util import host, say, torch_cuda
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": "float32", "bf16": "bfloat16", "f16": "float16"}
+U_OUT = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+
+
+def _km():
+    import paper_2608_14648_amd as km
+    return km
+
+
+def _fmt_dtype(torch, fmt):
+    return torch.int8 if fmt == "int8" else torch.float8_e4m3fn
+
+
+class Setup:
+    """A cache with garbage in it, on the GPU and in the oracle, and the sequences of a call."""
+
+    def __init__(self, fmt, page, heads, d, lens, rows, seed, spare=2, wide=0, shuffle=True):
+        import oracle.kv as okv
+        torch = torch_cuda()
+        km = _km()
+        self.torch, self.km, self.fmt = torch, km, fmt
+        rng = np.random.default_rng(seed)
+        self.rng = rng
+        per = [-(-l // page) for l in lens]
+        pages = sum(per) + spare
+        order = rng.permutation(pages) if shuffle else np.arange(pages)
+        width = max(max(per), 1) + wide
+        self.table = np.full((len(lens), width), -1, np.int32)
+        at = 0
+        for b, p in enumerate(per):
+            self.table[b, :p] = order[at:at + p]
+            at += p
+        self.lens = np.array(lens, np.int32)
+        self.starts = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+        self.rows, self.max_rows = int(self.starts[-1]), int(max(rows))
+        if fmt == "int8":
+            raw = rng.integers(-127, 128, (2, pages, heads, page, d)).astype(np.int8)
+            val = raw.astype(np.float64)
+        else:
+            raw = rng.integers(0, 256, (2, pages, heads, page, d)).astype(np.uint8)
+            raw[(raw & 127) == 127] ^= 1  # no NaN
+            val = okv.e4m3_values()[raw]
+        mul = okv.short(np.exp(rng.normal(3.0, 0.4, (2, pages, heads))).astype(np.float32))
+        self.orc = okv.Cache(fmt, val[0], np.swapaxes(val[1], 2, 3), mul[0], mul[1])
+        dt = _fmt_dtype(torch, fmt)
+        k = torch.from_numpy(raw[0].view(np.int8).copy()).cuda().view(dt)
+        v = torch.from_numpy(np.ascontiguousarray(np.swapaxes(raw[1], 2, 3)).view(np.int8)).cuda().view(dt)
+        sc = torch.from_numpy(np.float32(1.0) / mul).cuda()
+        self.cache = km.KvCache(k, v, sc[0].contiguous(), sc[1].contiguous())
+        self.seqs = self.seqs_of(self.lens, self.starts)
+
+    def seqs_of(self, lens, starts, table=None):
+        torch = self.torch
+        t = torch.from_numpy(self.table if table is None else table).cuda()
+        return self.km.KvSeqs(t, torch.from_numpy(np.asarray(lens, np.int32)).cuda(),
+                              torch.from_numpy(np.asarray(starts, np.int32)).cuda(), rows=int(starts[-1]),
+                              max_rows=int(np.diff(starts).max()))
+
+    def normal(self, shape, type_, size=1.0):
+        x = self.torch.from_numpy((self.rng.standard_normal(shape) * size).astype(np.float32))
+        return x.to(getattr(self.torch, DT[type_])).cuda()
+
+    def values(self, which):
+        """Code values of the cache on the GPU, tokens before dims."""
+        t = (self.cache.k, self.cache.v)[which]
+        x = t.float().cpu().numpy().astype(np.float64)
+        return np.swapaxes(x, 2, 3) if which else x
+
+    def check_cache(self, label):
+        self.torch.cuda.synchronize()
+        for which, name in ((0, "k"), (1, "v")):
+            np.testing.assert_array_equal(self.values(which), self.orc.codes[which], err_msg=f"{label}: {name} codes")
+            sc = host((self.cache.k_scale, self.cache.v_scale)[which])
+            np.testing.assert_array_equal(sc, self.orc.scales(which), err_msg=f"{label}: {name} scales")
+
+    def write(self, k, v, lens=None, starts=None):
+        lens = self.lens if lens is None else lens
+        starts = self.starts if starts is None else starts
+        self.km.kv_write(self.cache, self.seqs_of(lens, starts), k, v)
+        f = [x.float().cpu().numpy().astype(np.float64) for x in (k, v)]
+        self.orc.write(self.table, lens, starts, *f)
+
+
+WRITES = [
+    # page, heads, d, lens, rows
+    (16, 1, 16, [1], [1]),
+    (16, 2, 64, [1, 16, 17, 40], [1, 16, 2, 40]),
+    (32, 3, 80, [33, 5, 64, 0], [1, 5, 33, 0]),
+    (64, 2, 128, [200, 64, 129], [137, 1, 129]),
+    (64, 1, 96, [63, 65, 128], [3, 20, 64]),
+    (128, 2, 256, [300, 127], [45, 127]),
+    (128, 1, 48, [129, 128], [17, 16]),
+]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("type_", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("case", range(len(WRITES)))
+def test_write_and_read_exact(fmt, type_, case):
+    page, heads, d, lens, rows = WRITES[case]
+    say(f"kv_write {fmt} {type_} page={page} heads={heads} d={d} lens={lens} rows={rows}")
+    s = Setup(fmt, page, heads, d, lens, rows, seed=100 + case)
+    shape = (s.rows, heads, d)
+    # rows of differing size, so that some open pages' scales grow and some do not
+    size = np.exp(s.rng.normal(0, 1.5, (s.rows, heads, 1)))
+    k, v = s.normal(shape, type_, size), s.normal(shape, type_, size)
+    s.write(k, v)
+    s.check_cache("write")
+    # read everything back
+    starts = np.concatenate([[0], np.cumsum(lens)])
+    gk, gv = s.km.kv_read(s.cache, s.seqs_of(lens, starts), k.dtype)
+    s.torch.cuda.synchronize()
+    for which, got in ((0, gk), (1, gv)):
+        sc = s.orc.scales(which)
+        want = np.zeros((int(starts[-1]), heads, d), np.float32)
+        for b, ln in enumerate(lens):
+            for j in range(ln):
+                pg = s.table[b, j // page]
+                want[starts[b] + j] = s.orc.codes[which][pg, :, j % page].astype(np.float32) * sc[pg][:, None]
+        top = s.torch.finfo(k.dtype).max
+        want = s.torch.from_numpy(want).clamp(-top, top).to(k.dtype)
+        np.testing.assert_array_equal(got.float().cpu().numpy(), want.float().numpy())
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+def test_write_token_by_token(fmt, type_):
+    """A page filled one token at a time, each a little larger or smaller: every step is the oracle's, growth included."""
+    page, heads, d, n = 16, 2, 32, 40
+    s = Setup(fmt, page, heads, d, [n, n], [1, 1], seed=7)
+    starts = np.array([0, 1, 2])
+    for t in range(1, n + 1):
+        size = 1.0 + 0.1 * t if t % 3 else 0.2
+        k, v = s.normal((2, heads, d), type_, size), s.normal((2, heads, d), type_, 3.0 - size / 2)
+        s.write(k, v, lens=np.array([t, t]), starts=starts)
+        s.check_cache(f"token {t}")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("type_", ["f32", "bf16", "f16"])
+def test_write_special_values(fmt, type_):
+    """Zeros, ties, subnormals, the type's largest value, infinities and NaN."""
+    torch = torch_cuda()
+    page, heads, d = 16, 1, 32
+    s = Setup(fmt, page, heads, d, [16] * 8, [16] * 8, seed=11)
+    dt = getattr(torch, DT[type_])
+    x = s.normal((128, heads, d), type_).cpu()
+    top, tiny = torch.finfo(dt).max, torch.finfo(dt).tiny
+    x[0:16] = 0.0
+    x[16:32] = torch.where(torch.arange(d) % 2 == 0, 0.5, 127.0).to(dt)  # 0.5 is a tie of int8 for amax 127
+    x[32:48] *= tiny
+    x[48:64] = top
+    x[49] = -top
+    x[70, 0, 3], x[71, 0, 4], x[72, 0, 5] = math.inf, -math.inf, math.nan
+    x[80:96] = math.nan
+    x[96:112] = math.inf
+    x[112:128] = torch.linspace(-127, 127, 16 * d).view(16, 1, d).to(dt)
+    x = x.cuda()
+    s.write(x, -x)
+    s.check_cache("special")
+    gk, _ = s.km.kv_read(s.cache, s.seqs, dt)
+    assert bool(torch.isfinite(gk.float()).all())
+
+
+def test_write_int8_at_the_last_bit_of_a_tie():
+    """fp32 values a last bit beside code + 1/2: the exact product decides, not the rounded one."""
+    torch = torch_cuda()
+    s = Setup("int8", 16, 1, 64, [16], [16], seed=3)
+    base = (np.arange(16 * 64 - 1) % 126 + 0.5).astype(np.float32)
+    x = np.empty(16 * 64, np.float32)
+    x[0] = 127.0 / 1.01171875  # the multiplier is no power of two: products need more bits than fp32 has
+    near = base / np.float32(1.01171875)
+    x[1:] = np.where(np.arange(len(base)) % 3 == 0, near, np.where(np.arange(len(base)) % 3 == 1,
+                     np.nextafter(near, np.float32(1e9)), np.nextafter(near, np.float32(0))))
+    t = torch.from_numpy(x.reshape(16, 1, 64)).cuda()
+    s.write(t, -t)
+    s.check_cache("ties")
+    s8 = Setup("fp8", 16, 1, 64, [16], [16], seed=3)
+    mid = np.array([8.5, 9.5, 17.0, 19.0, 100.0, 0.001953125 * 2.5])
+    y = np.resize(mid, 16 * 64).astype(np.float32) / np.float32(1.01171875)
+    y[::3] = np.nextafter(y[::3], np.float32(1e9))
+    y[1::3] = np.nextafter(y[1::3], np.float32(0))
+    y[0] = 448.0 / 1.01171875
+    t = torch.from_numpy(y.reshape(16, 1, 64)).cuda()
+    s8.write(t, -t)
+    s8.check_cache("ties fp8")
+
+
+def test_strided_rows_and_rows_before_the_start():
+    torch = torch_cuda()
+    heads, d = 2, 64
+    # sequence 1 has more rows than tokens: two of them fall before position 0
+    s = Setup("int8", 16, heads, d, [20, 3], [4, 5], seed=5)
+    fused = s.normal((s.rows, 3 * heads, d), "bf16")
+    k, v = fused[:, heads:2 * heads], fused[:, 2 * heads:]
+    s.write(k, v)
+    s.check_cache("strided")
+    buf = torch.full((s.rows, 2 * heads, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    s.km.kv_read(s.cache, s.seqs, k=buf[:, :heads], v=buf[:, heads:])
+    got = buf.float().cpu().numpy()
+    assert (got[4:6] == 0).all()  # the rows without a place
+    want = s.orc.rows(s.table[1], 0, 3)
+    np.testing.assert_array_equal(
+        got[6:9, :heads], torch.from_numpy(want[0].astype(np.float32)).bfloat16().float().numpy())
+    np.testing.assert_array_equal(
+        got[6:9, heads:], torch.from_numpy(want[1].astype(np.float32)).bfloat16().float().numpy())
+
+
+def _attend_check(s, q, type_, causal=True, window=0, scale=None, table=None, label=""):
+    torch, km = s.torch, s.km
+    scale = 1.0 / math.sqrt(s.orc.d) if scale is None else scale
+    seqs = s.seqs if table is None else s.seqs_of(s.lens, s.starts, table)
+    out, lse = km.kv_attend(s.cache, seqs, q, scale=scale, causal=causal, window=window, lse=True)
+    torch.cuda.synchronize()
+    out, lse = out.float().cpu().numpy().astype(np.float64), host(lse).astype(np.float64)
+    f32_scale = float(np.float32(scale))
+    o, L, av, big, most = s.orc.attend(s.table if table is None else table, s.lens, s.starts,
+                                 q.float().cpu().numpy(), f32_scale, causal, window)
+    d, N = s.orc.d, int(s.lens.max())
+    none = np.isneginf(L)
+    T = (big + np.where(none, 0, np.abs(L))) * 1.45 + 16 + 32  # exponents: scores, statistics, offset, scales
+    e = 2.0 ** -24 * (d * big + 4 * T + 8)
+    u_w = 2.0 ** -11
+    if type_ == "f32":
+        u_w = 2.0 ** -21
+        e = e + 2.0 ** -21 * big  # two halves of the queries
+    bound = U_OUT[type_] * np.abs(o) + ((u_w + 2 * (e + N * 2.0 ** -24))[..., None]) * av + (N * 2.0 ** -40 * most)[..., None] + 1e-30
+    bad = np.abs(out - o) - bound
+    assert (out[none] == 0).all() and np.isneginf(lse[none]).all(), label
+    assert bad.max() <= 0, f"{label}: off by {np.abs(out - o).flat[bad.argmax()]:.3e}, bound {bound.flat[bad.argmax()]:.3e}"
+    ok = ~none
+    gap = np.abs(lse[ok] - L[ok]) - (e[ok] + (N + 4 * np.abs(L[ok])) * 2.0 ** -24)
+    assert ok.sum() == 0 or gap.max() <= 0, f"{label}: lse off by {np.abs(lse[ok] - L[ok]).max():.3e}"
+    return out, lse
+
+
+ATTENDS = [
+    # page, heads, group, d, lens, rows, window
+    (16, 1, 1, 16, [1], [1], 0),
+    (16, 2, 1, 64, [1, 15, 16, 17, 63, 64, 65], [1] * 7, 0),
+    (16, 2, 4, 64, [100, 257, 31], [1, 1, 1], 0),
+    (64, 2, 4, 128, [777, 64, 1, 129], [1] * 4, 0),
+    (128, 1, 8, 128, [300, 1025], [1, 1], 0),
+    (32, 1, 16, 96, [333, 32], [1, 1], 0),
+    (32, 1, 5, 80, [70, 190], [1, 1], 0),
+    (64, 2, 2, 192, [129, 500], [1, 1], 0),
+    (64, 1, 4, 256, [65, 400], [1, 1], 0),
+    (64, 1, 32, 128, [260], [1], 0),
+    (16, 1, 1, 128, [2000], [1], 0),
+    (32, 2, 3, 112, [50, 40], [7, 40], 0),
+    (16, 1, 2, 240, [33, 64], [33, 20], 0),
+    (64, 2, 4, 128, [300, 90], [5, 90], 0),
+    (64, 1, 4, 64, [200, 130, 3], [130, 130, 3], 0),
+    (16, 1, 1, 128, [150], [150], 0),
+    (128, 1, 6, 128, [170, 301], [170, 63], 0),
+    (32, 1, 2, 128, [100, 400], [3, 70], 33),
+    (64, 2, 8, 128, [1000, 70], [4, 4], 64),
+    (64, 1, 1, 64, [500], [1], 1),
+    (64, 1, 4, 256, [150, 70], [150, 64], 50),
+]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("type_", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("case", range(len(ATTENDS)))
+def test_attend(fmt, type_, case):
+    page, heads, group, d, lens, rows, window = ATTENDS[case]
+    say(f"kv_attend {fmt} {type_} page={page} heads={heads}x{group} d={d} lens={lens} rows={rows} window={window}")
+    s = Setup(fmt, page, heads, d, lens, rows, seed=200 + case)
+    q = s.normal((s.rows, heads * group, d), type_, 0.6 if fmt == "int8" else 0.3)
+    _attend_check(s, q, type_, window=window, label="causal")
+    if not window:
+        _attend_check(s, q, type_, causal=False, label="whole")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_attend_rows_that_see_nothing(fmt, rows):
+    """Rows before position 0, empty sequences, pages that are not there: zeros and -inf, and nobody else is touched."""
+    s = Setup(fmt, 16, 1, 64, [0, 40, 100, 33], [rows, rows, rows, rows], seed=9, wide=2)
+    q = s.normal((s.rows, 4, 64), "bf16")
+    _attend_check(s, q, "bf16", label="short")
+    table = s.table.copy()
+    table[1, :] = -1
+    table[2, 1:3] = 10 ** 6
+    table[3, 0] = -5
+    _attend_check(s, q, "bf16", table=table, label="absent pages")
+    _attend_check(s, q, "bf16", table=table, causal=False, label="absent pages, whole")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("rows", [1, 40, 200])
+def test_attend_ignores_what_lies_behind_the_end(fmt, rows):
+    """Codes and scales behind the end of a sequence (NaN codes, NaN and huge scales) change nothing."""
+    torch = torch_cuda()
+    s = Setup(fmt, 16, 2, 64, [200, 217, 210], [rows, rows, rows], seed=13, wide=5)
+    q = s.normal((s.rows, 4, 64), "f16")
+    a, la = s.km.kv_attend(s.cache, s.seqs, q, lse=True)
+    k, v = s.cache.k.view(torch.uint8), s.cache.v.view(torch.uint8)
+    used = np.zeros((s.cache.pages, 16), bool)
+    for b, ln in enumerate(s.lens):
+        for j in range(ln):
+            used[s.table[b, j // 16], j % 16] = True
+    free = torch.from_numpy(~used).cuda()
+    k[free[:, None, :, None].expand(k.shape)] = 0x7F
+    v[free[:, None, None, :].expand(v.shape)] = 0xFF
+    lost = torch.from_numpy(~used.any(1)).cuda()
+    s.cache.k_scale[lost] = math.nan
+    s.cache.v_scale[lost] = 3e38
+    b, lb = s.km.kv_attend(s.cache, s.seqs, q, lse=True)
+    assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+@pytest.mark.parametrize("rows", [1, 64])
+@pytest.mark.parametrize("type_", ["bf16", "f32"])
+def test_attend_scales_far_apart(rows, type_):
+    """Pages whose scales differ by many powers of two, tiny and huge queries."""
+    torch = torch_cuda()
+    import oracle.kv as okv
+    s = Setup("int8", 16, 1, 64, [150, 100], [rows, rows], seed=17)
+    mul = okv.short(np.exp2(s.rng.uniform(-8, 40, (2, s.cache.pages, 1))).astype(np.float32))
+    s.orc.mul = [mul[0], mul[1]]
+    s.cache.k_scale.copy_(torch.from_numpy(s.orc.scales(0)))
+    s.cache.v_scale.copy_(torch.from_numpy(s.orc.scales(1)))
+    for size in (1e-30, 1e-3, 1.0):
+        q = s.normal((s.rows, 2, 64), type_, size * 0.01)
+        _attend_check(s, q, type_, label=f"size {size}")
+
+
+@pytest.mark.parametrize("rows", [1, 64])
+def test_attend_not_finite_queries_stay_in_their_row(rows):
+    torch = torch_cuda()
+    s = Setup("int8", 16, 1, 64, [90, 100], [rows, rows], seed=19)
+    q = s.normal((s.rows, 4, 64), "bf16")
+    good, _ = s.km.kv_attend(s.cache, s.seqs, q)
+    bad = q.clone()
+    bad[0, 1, 5] = math.nan
+    bad[rows, 2, 6] = math.inf
+    got, _ = s.km.kv_attend(s.cache, s.seqs, bad)
+    touched = torch.zeros(q.shape[:2], dtype=torch.bool, device="cuda")
+    touched[0, 1] = touched[rows, 2] = True
+    assert torch.equal(got[~touched], good[~touched])
+    assert bool(torch.isnan(got[0, 1]).all())
+
+
+def test_invalid_sequences_are_left_alone():
+    """Lengths and row ranges that do not fit the call: their rows keep their contents, the others are right."""
+    torch = torch_cuda()
+    km = _km()
+    s = Setup("int8", 16, 1, 64, [40, 40, 40, 40], [2, 2, 2, 2], seed=23)
+    q = s.normal((8, 2, 64), "bf16")
+    want, _ = km.kv_attend(s.cache, s.seqs, q)
+    t = torch.from_numpy(s.table).cuda()
+    lens = torch.tensor([40, -1, 10 ** 6, 40], dtype=torch.int32, device="cuda")
+    seqs = km.KvSeqs(t, lens, torch.tensor([0, 2, 4, 6, 8], dtype=torch.int32, device="cuda"), rows=8, max_rows=2)
+    out = torch.full_like(q, 3.0)
+    km.kv_attend(s.cache, seqs, q, out=out)
+    assert torch.equal(out[:2], want[:2]) and torch.equal(out[6:], want[6:]) and bool((out[2:6] == 3).all())
+    starts = torch.tensor([0, 2, 5, 6, 9], dtype=torch.int32, device="cuda")  # three rows; past the last row
+    lens = torch.full((4,), 40, dtype=torch.int32, device="cuda")
+    seqs = km.KvSeqs(t, lens, starts, rows=8, max_rows=2)
+    out = torch.full_like(q, 3.0)
+    km.kv_attend(s.cache, seqs, q, out=out)
+    assert torch.equal(out[:2], want[:2]) and bool((out[2:5] == 3).all()) and bool((out[6:] == 3).all())
+    before = [x.clone() for x in (s.cache.k, s.cache.v, s.cache.k_scale, s.cache.v_scale)]
+    bad = km.KvSeqs(t, torch.full((4,), -3, dtype=torch.int32, device="cuda"), None, rows=8)
+    kv = s.normal((8, 1, 64), "bf16")
+    km.kv_write(s.cache, bad, kv, kv)
+    for a, b in zip(before, (s.cache.k, s.cache.v, s.cache.k_scale, s.cache.v_scale)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_other_stream_repeats_and_graph():
+    """The same bits on another stream, on every repeat, and from a captured graph between eager work."""
+    torch = torch_cuda()
+    km = _km()
+    s = Setup("int8", 64, 2, 128, [3000, 500], [1, 1], seed=29)
+    q = s.normal((2, 8, 128), "bf16")
+    want, lw = km.kv_attend(s.cache, s.seqs, q, lse=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got, lg = km.kv_attend(s.cache, s.seqs, q, lse=True)
+    side.synchronize()
+    assert torch.equal(got, want) and torch.equal(lg, lw)
+    new = s.normal((2, 2, 128), "bf16")
+    out = torch.empty_like(q)
+    with torch.cuda.stream(side):
+        km.kv_write(s.cache, s.seqs, new, new)
+        km.kv_attend(s.cache, s.seqs, q, out=out)
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        km.kv_write(s.cache, s.seqs, new, new)
+        km.kv_attend(s.cache, s.seqs, q, out=out)
+    for i in range(4):
+        q.copy_(s.normal((2, 8, 128), "bf16"))
+        new.copy_(s.normal((2, 2, 128), "bf16", 1.0 + i))
+        before = [x.clone() for x in (s.cache.k, s.cache.v, s.cache.k_scale, s.cache.v_scale)]
+        g.replay()
+        torch.cuda.synchronize()
+        replayed = out.clone()
+        for a, b in zip((s.cache.k, s.cache.v, s.cache.k_scale, s.cache.v_scale), before):
+            a.copy_(b)
+        km.kv_write(s.cache, s.seqs, new, new)
+        eager, _ = km.kv_attend(s.cache, s.seqs, q)
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, eager), i
+
+
+def test_offsets_past_32_bits():
+    """A cache of more than 4 GiB per codes tensor: the last pages are read and written where they lie."""
+    torch = torch_cuda()
+    km = _km()
+    heads, page, d = 8, 128, 256
+    pages = (1 << 32) // (heads * page * d) + 40
+    k = torch.zeros((pages, heads, page, d), dtype=torch.int8, device="cuda")
+    v = torch.zeros((pages, heads, d, page), dtype=torch.int8, device="cuda")
+    sc = torch.ones((pages, heads), dtype=torch.float32, device="cuda")
+    cache = km.KvCache(k, v, sc, sc.clone())
+    small = km.kv_cache(4, heads, d, page)
+    big_t = torch.tensor([[pages - 1, 3, pages - 2]], dtype=torch.int32, device="cuda")
+    small_t = torch.tensor([[0, 1, 2]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([300], dtype=torch.int32, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(300, heads, d, generator=g, device="cuda").bfloat16()
+    q = torch.randn(300, heads, d, generator=g, device="cuda").bfloat16()
+    res = []
+    for c, t in ((cache, big_t), (small, small_t)):
+        seqs = km.KvSeqs(t, lens, None, rows=300)
+        km.kv_write(c, seqs, x, x * 0.5)
+        one = km.KvSeqs(t, lens)
+        res.append([*km.kv_read(c, seqs), km.kv_attend(c, seqs, q)[0], km.kv_attend(c, one, q[:1].contiguous())[0]])
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
