@@ -32,8 +32,10 @@ struct AttendArgs {
   KvSeqs S;
   KvAttend A;
   int rtiles;  // row tiles per sequence and head
-  int splits;
-  float *part;  // splits > 1: [tile][split] blocks of accumulators, then M and l
+  int deal;     // tiles are dealt out (kv_attend_kernel)
+  int splits;   // the most that a tile is split into; if dealt out, workgroups
+  int per;      // chunks of a split or, at least, of a workgroup
+  float *part;  // blocks of accumulators, then M and l: [tile][split], or if dealt out two for each workgroup
 };
 
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
@@ -53,11 +55,33 @@ __device__ __forceinline__ float sum_groups(float x) {
 // the 16 rows.
 __host__ __device__ constexpr int part_floats(int nt) { return nt * 256 + 32; }
 
-// 16 values of a row as fp32, whatever their type (dims from c on; c + 16 <= d)
-__device__ __forceinline__ void load_q16(const KvAttend &A, int64_t o, float *x) {
-  if (A.type == KM_T_F32) kv_load<KM_T_F32, 16>(A.q.p, o, x);
-  else if (A.type == KM_T_BF16) kv_load<KM_T_BF16, 16>(A.q.p, o, x);
-  else kv_load<KM_T_F16, 16>(A.q.p, o, x);
+// 16 values of a row as fp32: N = 2 * NS groups of 16 bytes, fp32 ones (NS = 2) or of the type.
+template <int NS>
+__device__ __forceinline__ void values16(const u32x4 *raw, int type, float *x) {
+  if constexpr (NS == 2) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(raw[i / 4][i % 4]);
+  } else if (type == KM_T_BF16) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t w = raw[i / 8][i / 2 % 4];
+      x[i] = __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t w = raw[i / 8][i / 2 % 4];
+      x[i] = (float)__builtin_bit_cast(f16x2, w)[i % 2];
+    }
+  }
+}
+template <int NS>
+__device__ __forceinline__ float top16(const u32x4 *raw, int type) {
+  float v[16], top = 0.0f;
+  values16<NS>(raw, type, v);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(v[i]));
+  return top;
 }
 
 __device__ __forceinline__ void store_o4(const KvAttend &A, int64_t o, const float *x) {
@@ -97,73 +121,204 @@ __device__ __forceinline__ void row_span(const KvAttend &A, const KvSeq &q, int 
   *lo = A.window ? max(pos + 1 - A.window, 0) : 0;
 }
 
-template <int FMT, int NT, int RT, int NS>
-__global__ __launch_bounds__(256) void kv_attend_kernel(AttendArgs P) {
+// Chunks [cb, ce) of a split of rows [r0, r1), and how many splits these rows have: as many as their positions need,
+// P.per chunks each, one if they see none.  False: no such split.
+__device__ __forceinline__ bool tile_span(const AttendArgs &P, const KvSeq &q, int r0, int r1, int split, int *cb, int *ce,
+                                          int *splits) {
+  int lo, hi, any;
+  row_span(P.A, q, r0, &lo, &any);      // the first row's first position
+  row_span(P.A, q, r1 - 1, &any, &hi);  // the last row's last
+  const int c0 = lo / kChunk, n = hi > lo ? (hi + kChunk - 1) / kChunk - c0 : 0;
+  *splits = min(max((n + P.per - 1) / P.per, 1), P.splits);
+  const int per = (n + *splits - 1) / *splits;
+  *cb = c0 + split * per;
+  *ce = min(*cb + per, c0 + n);
+  return split < *splits;
+}
+
+// Dealing out.  The chunks of all tiles of a call, one sequence after the other, are cut into equal runs, a run for each
+// workgroup, so that every workgroup streams as many bytes as the others whatever the lengths are.  A tile counts kTileCost
+// chunks more than it has, about what a workgroup loses at its beginning and end.
+constexpr int kTileCost = 8;
+
+// The chunks that a sequence's rows see, in all of its tiles alike: [c0, c0 + n).
+struct SeqChunks {
+  int c0, n, tiles;
+  int cost;  // of all its tiles
+};
+__device__ __forceinline__ SeqChunks seq_chunks(const AttendArgs &P, int b, int trows, KvSeq *q) {
+  SeqChunks s{0, 0, 0, 0};
+  if (!kv_seq(P.S, P.C.page, b, q) || q->n == 0) return s;
+  int lo, hi, any;
+  const int rows = q->n * P.A.group;
+  row_span(P.A, *q, 0, &lo, &any);
+  row_span(P.A, *q, rows - 1, &any, &hi);
+  s.c0 = lo / kChunk;
+  s.n = max(hi > lo ? (hi + kChunk - 1) / kChunk - s.c0 : 0, 1);  // rows that see nothing take a chunk all the same
+  s.tiles = P.C.heads * ((rows + trows - 1) / trows);
+  s.cost = s.tiles * (s.n + kTileCost);
+  return s;
+}
+
+// Every wave goes through the sequences by itself, one per lane (the host deals only calls whose cost fits).
+struct DealScan {
+  int all;           // cost up to and including these 64 sequences
+  int before, cost;  // of this lane's sequence
+};
+__device__ __forceinline__ DealScan deal_scan(const AttendArgs &P, int trows, int b0, int all) {
+  const int lane = threadIdx.x & 63;
+  KvSeq q;
+  const int w = b0 + lane < P.S.n ? seq_chunks(P, b0 + lane, trows, &q).cost : 0;
+  int sum = w;  // of the lanes up to this one
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int y = __shfl_up(sum, o);
+    if (lane >= o) sum += y;
+  }
+  return {all + __builtin_amdgcn_readlane(sum, 63), all + sum - w, w};
+}
+// the cost of the call; the scan of its last 64 sequences
+__device__ __forceinline__ DealScan deal_all(const AttendArgs &P, int trows) {
+  DealScan s{0, 0, 0};
+  for (int b0 = 0; b0 < P.S.n; b0 += 64) s = deal_scan(P, trows, b0, s.all);
+  return s;
+}
+// the cost of the sequences before b
+__device__ __forceinline__ int deal_before(const AttendArgs &P, int trows, DealScan s, int b) {
+  const int last = (P.S.n - 1) & ~63;
+  if (b < last) {
+    s.all = 0;
+    for (int b0 = 0; b0 <= b; b0 += 64) s = deal_scan(P, trows, b0, s.all);
+  }
+  return __builtin_amdgcn_readlane(s.before, b & 63);
+}
+// the sequence that holds place `at`, and the cost of those before it
+__device__ __forceinline__ int deal_find(const AttendArgs &P, int trows, DealScan s, int at, int *before) {
+  int b0 = (P.S.n - 1) & ~63;
+  uint64_t hit = __ballot(at >= s.before && at < s.before + s.cost);
+  if (!hit) {
+    s.all = 0;
+    for (b0 = -64; !hit && b0 + 64 < P.S.n;) {
+      b0 += 64;
+      s = deal_scan(P, trows, b0, s.all);
+      hit = __ballot(at >= s.before && at < s.before + s.cost);
+    }
+  }
+  const int y = __ffsll((long long)hit) - 1;
+  *before = __builtin_amdgcn_readlane(s.before, y);
+  return b0 + y;
+}
+// the cost that a workgroup takes
+__device__ __forceinline__ int deal_run(const AttendArgs &P, int all) {
+  return max((int)(((uint32_t)all + P.splits - 1) / (uint32_t)P.splits), P.per);
+}
+
+constexpr int kAttendWaves = 4;
+
+// LDS of a workgroup: maxima and sums of each wave's rows, then each wave's accumulators.
+template <int RT, int NT>
+struct AttendWave {
+  float m[RT][16], l[RT][16];
+  f32x4 o[RT * NT][64];
+};
+
+// Chunks [cb, ce) of rows [r0, ...) of a sequence's head; the results, or where part is given the sums for the join.
+template <int FMT, int NT, int RT, int NS, bool ONE>
+__device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q, int b, int h, int r0, int cb, int ce,
+                                            float *part, AttendWave<RT, NT> *sh) {
   constexpr int NP = (NT + 3) / 4;  // groups of 64 dims
-  __shared__ float sh_m[4][RT][16], sh_l[4][RT][16];
-  __shared__ f32x4 sh_o[2][RT * NT][64];
+  constexpr int W = kAttendWaves;
   const KvCache &C = P.C;
   const KvAttend &A = P.A;
-  int64_t x = blockIdx.x;
-  const int split = (int)(x % P.splits);
-  x /= P.splits;
-  const int64_t tile = x;
-  const int rt = (int)(x % P.rtiles);
-  x /= P.rtiles;
-  const int h = (int)(x % C.heads);
-  const int b = (int)(x / C.heads);
-  KvSeq q;
-  if (!kv_seq(P.S, C.page, b, &q)) return;
-  const int rows = q.n * A.group, r0 = rt * 16 * RT;
-  if (r0 >= rows) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  const int d = C.d;
+  const int d = C.d, rows = q.n * A.group;
 
-  // the rows of this lane (rows past the last repeat it and are not stored), their scale and their spans
+  // Codes of a chunk.  Its page (ONE), or the pages of this lane's runs of 16: keys of run kr, values of run g.  Behind the
+  // end and where a page is not there something of the cache is read that counts for nothing.
+  const int64_t hb = (int64_t)C.page * d;  // bytes of a page's head
+  const int pmask = C.page - 1, last = max(q.len - 1, 0);
+  const int *table = P.S.table + (int64_t)b * P.S.table_ld;
+  const int kr = m >> 2, ktok = m & 3;
+  auto page_of = [&](int j) {
+    const int pg = table[min(j, last) >> C.shift];
+    return ONE ? __builtin_amdgcn_readfirstlane(pg) : pg;
+  };
+  auto page_at = [&](int pg) { return (int64_t)(pg >= 0 && pg < C.pages ? pg : 0) * C.heads + h; };
+  int pk, pv;
+  auto pages = [&](int c) {
+    pv = page_of(c * kChunk + (ONE ? 0 : 16 * g));
+    pk = ONE ? pv : page_of(c * kChunk + 16 * kr);
+  };
+  u32x4 kw[4][NP], vw[NT];
+  float ks, vs;
+  bool there;
+  auto load_keys = [&](int c) {
+    const int tk = c * kChunk + (ONE ? 0 : 16 * kr);
+    const uint8_t *kp = C.k + page_at(pk) * hb + (tk & pmask) * d;
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        kw[st][p] = *reinterpret_cast<const u32x4 *>(
+            kp + 4 * st * d + (uint32_t)(((ONE ? 16 * kr : 0) + ktok) * d + min(64 * p + 16 * g, d - 16)));
+  };
+  auto load_values = [&](int c) {
+    const int tv = c * kChunk + (ONE ? 0 : 16 * g);
+    const int64_t at = page_at(pv);
+    there = c * kChunk + 16 * g < q.len && pv >= 0 && pv < C.pages;
+    const uint8_t *vp = C.v + at * hb + (tv & pmask);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+      vw[n] = *reinterpret_cast<const u32x4 *>(vp + min(16 * n, d - 16) * C.page +
+                                               (uint32_t)(m * C.page + (ONE ? 16 * g : 0)));
+    ks = C.ks[at];
+    vs = C.vs[at];
+  };
+  int c = cb + wave;
+  if (c < ce) {
+    pages(c);
+    load_keys(c);
+    load_values(c);
+    if (c + W < ce) pages(c + W);
+  }
+
+  // the rows of this lane (rows past the last repeat it and are not stored), their scale and their spans; dims past d are 0
   f16x8 qf[RT][NP][2][NS];
   float cs[RT];
   int lo[RT], hi[RT];
+  u32x4 raw[RT][NP][2 * NS];  // 16 values each
 #pragma unroll
   for (int u = 0; u < RT; ++u) {
     const int r = min(r0 + 16 * u + m, rows - 1);
     row_span(A, q, r, &lo[u], &hi[u]);
-    const int64_t at = row_at(A, C, q, h, r).q;
-    float v[NP][16];
-    float top = 0.0f;
-#pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int c = 64 * p + 16 * g;
-      if (c < d) {
-        load_q16(A, at + c, v[p]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[p][i] = 0.0f;
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(v[p][i]));
-    }
-    top = max_groups(top);
-    float f;
-    q_scale(top, A.scale, &f, &cs[u]);
+    const char *at = static_cast<const char *>(A.q.p) + row_at(A, C, q, h, r).q * (2 * NS);
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float y = v[p][8 * k + i] * f;
-          const _Float16 hi16 = (_Float16)y;
-          qf[u][p][k][0][i] = hi16;
-          if constexpr (NS == 2) qf[u][p][k][1][i] = (_Float16)(y - (float)hi16);
-        }
+      for (int i = 0; i < 2 * NS; ++i)
+        raw[u][p][i] = reinterpret_cast<const u32x4 *>(at + min(64 * p + 16 * g, d - 16) * (2 * NS))[i];
   }
-  // the tile's positions: from the first row's first to the last row's last
-  int jlo, jhi, any;
-  row_span(A, q, r0, &jlo, &any);
-  row_span(A, q, min(r0 + 16 * RT, rows) - 1, &any, &jhi);
-  const int c0 = jlo / kChunk, c1 = jhi > jlo ? (int)cdiv(jhi, kChunk) : c0;
-  const int per = (c1 - c0 + P.splits - 1) / P.splits;
-  const int cb = c0 + split * per, ce = min(cb + per, c1);
+#pragma unroll
+  for (int u = 0; u < RT; ++u) {
+    float top = 0.0f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) top = fmaxf(top, top16<NS>(raw[u][p], A.type));
+    float f;
+    q_scale(max_groups(top), A.scale, &f, &cs[u]);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const float fp = 64 * p + 16 * g < d ? f : 0.0f;
+      float v[16];
+      values16<NS>(raw[u][p], A.type, v);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = fp == 0.0f ? 0.0f : v[i] * fp;
+        const _Float16 y16 = (_Float16)y;
+        qf[u][p][i / 8][0][i % 8] = y16;
+        if constexpr (NS == 2) qf[u][p][i / 8][1][i % 8] = (_Float16)(y - (float)y16);
+      }
+    }
+  }
 
   f32x4 acc[RT][NT];
   float M[RT], l[RT];
@@ -175,39 +330,15 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(AttendArgs P) {
     for (int n = 0; n < NT; ++n) acc[u][n] = f32x4{0, 0, 0, 0};
   }
 
-  const int64_t hb = (int64_t)C.page * d;  // bytes of a page's head
-  const int pmask = C.page - 1;
-  const int *table = P.S.table + (int64_t)b * P.S.table_ld;
-  const int kr = m >> 2;                 // this lane's key rows lie in 16-token run kr, its values in run g
-  const int ktok = m & 3;
-  for (int c = cb + wave; c < ce; c += 4) {
+  // The registers of a chunk's keys are loaded again as soon as its scores are done, those of its values after the second
+  // product: each load has half a step to arrive.
+  for (; c < ce; c += W) {
     const int j0 = c * kChunk;
-    // pages of the runs: past the sequence's end or outside the cache, page 0 is read and nothing of it counts
-    const int tk = j0 + 16 * kr, tv = j0 + 16 * g;
-    int64_t pk = tk < q.len ? table[tk >> C.shift] : 0;
-    int64_t pv = tv < q.len ? table[tv >> C.shift] : -1;
-    pk = pk >= 0 && pk < C.pages ? pk : 0;
-    const bool there = pv >= 0 && pv < C.pages;
-    pv = there ? pv : 0;
-    const uint8_t *kp = C.k + (pk * C.heads + h) * hb + (int64_t)((tk & pmask) + ktok) * d;
-    const uint8_t *vp = C.v + (pv * C.heads + h) * hb + (tv & pmask);
-    const float ks = there ? C.ks[pv * C.heads + h] : 1.0f;
-    const float vs = there ? C.vs[pv * C.heads + h] : 1.0f;
-
-    u32x4 kw[4][NP];
-#pragma unroll
-    for (int st = 0; st < 4; ++st)
-#pragma unroll
-      for (int p = 0; p < NP; ++p)
-        kw[st][p] = *reinterpret_cast<const u32x4 *>(kp + 4 * st * d + min(64 * p + 16 * g, d - 16));
-    u32x4 vw[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-      vw[n] = *reinterpret_cast<const u32x4 *>(vp + (int64_t)min(16 * n + m, d - 1) * C.page);
-
+    const bool more = c + W < ce;
     f32x4 s[RT][4];
 #pragma unroll
     for (int st = 0; st < 4; ++st) {
+      __builtin_amdgcn_sched_barrier(0);  // no more codes widened at a time than these products take
 #pragma unroll
       for (int u = 0; u < RT; ++u) s[u][st] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -221,18 +352,21 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(AttendArgs P) {
             for (int z = 0; z < NS; ++z) s[u][st] = mfma16(kf, qf[u][p][k][z], s[u][st]);
         }
     }
+    if (more) load_keys(c + W);
 
-    const float lv = __builtin_amdgcn_logf(vs), inv = 1.0f / vs;
+    const float k1 = there ? ks : 1.0f, v1 = there ? vs : 1.0f;
+    const float lv = __builtin_amdgcn_logf(v1), inv = 1.0f / v1;
     f16x8 w[RT][2][NS];
 #pragma unroll
     for (int u = 0; u < RT; ++u) {
-      const bool whole = __all(there && j0 >= lo[u] && j0 + kChunk <= hi[u]);
-      if (!whole) {
+      if (!__all(there && j0 >= lo[u] && j0 + kChunk <= hi[u])) {
+        int jg = j0 + 16 * g;
+        asm volatile("" : "+v"(jg));  // a branch: few chunks need it, so nothing of it is kept in registers
 #pragma unroll
         for (int st = 0; st < 4; ++st)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int j = tv + 4 * st + i;
+            const int j = jg + 4 * st + i;
             if (!there || j < lo[u] || j >= hi[u]) s[u][st][i] = -INFINITY;
           }
       }
@@ -241,9 +375,9 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(AttendArgs P) {
       for (int st = 0; st < 4; ++st)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[u][st][i]);
-      const float ck = cs[u] * ks;
-      const float t = top == -INFINITY ? -INFINITY : fmaf(top, ck, lv);
-      const float Mn = fmaxf(M[u], max_groups(t));
+      // a factor of 0 (a row of tiny queries) would make NaN of -inf
+      const float ck = fmaxf(cs[u] * k1, 0x1p-126f);
+      const float Mn = fmaxf(M[u], max_groups(fmaf(top, ck, lv)));
       if (__any(Mn > M[u])) {
         const float al = Mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(M[u] - Mn);
         l[u] *= al;
@@ -257,8 +391,7 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(AttendArgs P) {
       for (int st = 0; st < 4; ++st)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float y = __builtin_amdgcn_exp2f(fmaf(s[u][st][i], ck, base));
-          if (!whole && s[u][st][i] == -INFINITY) y = 0.0f;
+          const float y = __builtin_amdgcn_exp2f(fmaf(s[u][st][i], ck, base));
           sum += y;
           const _Float16 y16 = (_Float16)y;
           w[u][st / 2][0][4 * (st % 2) + i] = y16;
@@ -267,8 +400,9 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(AttendArgs P) {
       l[u] = fmaf(sum, inv, l[u]);
     }
     if constexpr (FMT == KM_KV_F8) {  // codes past the end may be NaN, which no weight of 0 takes out
-      if (j0 + kChunk > q.len || !__all(there)) {
-        const int left = there ? q.len - tv : 0;
+      if (!__all(there && j0 + kChunk <= q.len)) {
+        int left = there ? q.len - j0 - 16 * g : 0;
+        asm volatile("" : "+v"(left));
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -279,7 +413,8 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(AttendArgs P) {
       }
     }
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int n = 0; n < NT; ++n) {
+      if (n % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const f16x8 vf = kv_widen8<FMT>(vw[n][2 * k], vw[n][2 * k + 1]);
@@ -288,127 +423,241 @@ __global__ __launch_bounds__(256) void kv_attend_kernel(AttendArgs P) {
 #pragma unroll
           for (int z = 0; z < NS; ++z) acc[u][n] = mfma16(vf, w[u][k][z], acc[u][n]);
       }
+    }
+    if (more) {
+      load_values(c + W);
+      if (c + 2 * W < ce) pages(c + 2 * W);
+    }
   }
 
-  // the four waves' results: weights of a common maximum, then sums over the waves
+  // the waves' results: scaled to a common maximum, then each wave adds up its share of the accumulators, in the waves' order
 #pragma unroll
   for (int u = 0; u < RT; ++u) {
     l[u] = sum_groups(l[u]);
     if (l[u] != l[u]) M[u] = INFINITY;  // the maximum does not see NaN: the row's results are NaN from here
     if (g == 0) {
-      sh_m[wave][u][m] = M[u];
-      sh_l[wave][u][m] = l[u];
+      sh[wave].m[u][m] = M[u];
+      sh[wave].l[u][m] = l[u];
     }
   }
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < RT; ++u) {
-    const float Mx = fmaxf(fmaxf(sh_m[0][u][m], sh_m[1][u][m]), fmaxf(sh_m[2][u][m], sh_m[3][u][m]));
-    float sum = 0.0f;
+    float Mx = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      const float My = sh_m[y][u][m];
-      // a wave whose maximum is -inf has nothing; NaN stays NaN
-      sum += My == -INFINITY ? 0.0f : sh_l[y][u][m] * __builtin_amdgcn_exp2f(My - Mx);
+    for (int y = 0; y < W; ++y) Mx = fmaxf(Mx, sh[y].m[u][m]);
+#pragma unroll
+    for (int y = 0; y < W; ++y) {
+      const float My = sh[y].m[u][m];  // -inf: the wave has nothing
+      sum += My == -INFINITY ? 0.0f : sh[y].l[u][m] * __builtin_amdgcn_exp2f(My - Mx);
     }
     const float al = M[u] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[u] - Mx);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[u][n] *= al;
+    for (int n = 0; n < NT; ++n) sh[wave].o[u * NT + n][lane] = acc[u][n] * al;
     M[u] = Mx;
     l[u] = sum;
   }
-  if (wave & 1) {
-#pragma unroll
-    for (int u = 0; u < RT; ++u)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) sh_o[wave >> 1][u * NT + n][lane] = acc[u][n];
-  }
   __syncthreads();
-  if (!(wave & 1)) {
 #pragma unroll
-    for (int u = 0; u < RT; ++u)
+  for (int u = 0; u < RT; ++u) {
+    const int r = r0 + 16 * u + m;
+    if (r >= rows) continue;
+    const RowAt at = row_at(A, C, q, h, r);
+    const float inv = l[u] == 0.0f ? 0.0f : 1.0f / l[u];
+    float *o = part + u * part_floats(NT);
+    for (int n = wave; n < NT; n += W) {
+      f32x4 v = sh[0].o[u * NT + n][lane];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) acc[u][n] += sh_o[wave >> 1][u * NT + n][lane];
+      for (int y = 1; y < W; ++y) v += sh[y].o[u * NT + n][lane];
+      if (part) {
+        *reinterpret_cast<f32x4 *>(o + (n * 64 + lane) * 4) = v;
+      } else {
+        const int i0 = 16 * n + 4 * g;
+        v *= inv;
+        const float y[4] = {v.x, v.y, v.z, v.w};
+        if (i0 < d) store_o4(A, at.o + i0, y);
+      }
+    }
+    if (wave == 0 && g == 0) {
+      if (part) {
+        o[NT * 256 + m] = M[u];
+        o[NT * 256 + 16 + m] = l[u];
+      } else if (A.lse) {
+        A.lse[at.lse] = log_sum(M[u], l[u]);
+      }
+    }
   }
-  __syncthreads();
-  if (wave == 2) {
+}
+
+template <int FMT, int NT, int RT, int NS, bool ONE>
+__global__ __launch_bounds__(64 * kAttendWaves, NT <= 8 ? 2 : 1) void kv_attend_kernel(AttendArgs P) {
+  __shared__ AttendWave<RT, NT> sh[kAttendWaves];
+  constexpr int TR = 16 * RT;
+  KvSeq q;
+  if (!P.deal) {  // a workgroup per tile and split
+    const uint32_t splits = max(P.splits, 1);
+    uint32_t x = blockIdx.x / splits;
+    const int split = (int)(blockIdx.x - x * splits);
+    float *part = P.part + (int64_t)blockIdx.x * RT * part_floats(NT);
+    const int rt = (int)(x % (uint32_t)P.rtiles);
+    x /= (uint32_t)P.rtiles;
+    const int h = (int)(x % (uint32_t)P.C.heads), b = (int)(x / (uint32_t)P.C.heads);
+    if (!kv_seq(P.S, P.C.page, b, &q)) return;
+    const int r0 = rt * TR, rows = q.n * P.A.group;
+    int cb, ce, of;
+    if (r0 < rows && tile_span(P, q, r0, min(r0 + TR, rows), split, &cb, &ce, &of))
+      attend_tile<FMT, NT, RT, NS, ONE>(P, q, b, h, r0, cb, ce, of > 1 ? part : nullptr, sh);
+    return;
+  }
+  const DealScan o = deal_all(P, TR);
+  const int run = deal_run(P, o.all);
+  if ((int64_t)run * blockIdx.x >= o.all) return;
+  int at = run * (int)blockIdx.x, left = min(run, o.all - at), before;  // the place, and what is left to take
+  int b = deal_find(P, TR, o, at, &before);
+  at -= before;
+  for (; left > 0; ++b) {
+    const SeqChunks s = seq_chunks(P, b, TR, &q);
+    const int cost = s.n + kTileCost, rtiles = s.tiles / P.C.heads;
+    int tile = s.n ? (int)((uint32_t)at / (uint32_t)cost) : 0, skip = at - tile * cost;
+    at = 0;
+    for (; tile < s.tiles && left > 0; ++tile) {
+      const int take = min(left, cost - skip);
+      const int c0 = max(skip - kTileCost, 0), c1 = skip + take - kTileCost;
+      if (c1 > c0) {
+        // a tile that began in another workgroup, or one that is not finished here
+        float *part = c1 - c0 == s.n ? nullptr
+                                     : P.part + ((int64_t)blockIdx.x * 2 + (c0 == 0)) * RT * part_floats(NT);
+        attend_tile<FMT, NT, RT, NS, ONE>(P, q, b, tile / rtiles, tile % rtiles * TR, s.c0 + c0, s.c0 + c1, part, sh);
+      }
+      left -= take;
+      skip = 0;
+    }
+  }
+}
+
+// Joins the splits of R = 64 / G rows (G = 4: tiles of kv_attend_kernel, G = 2: of kv_prompt_kernel, whose accumulators lie
+// the same way).  DEAL: the blocks are those of the workgroups that the tile was dealt to.  spread: a workgroup per
+// accumulator of a lane, whose waves take the splits in turn and are added up in their order (few tiles, many splits);
+// otherwise one for all of them, whose waves take the accumulators in turn.
+constexpr int kJoinWaves = 8;
+
+struct JoinSum {
+  float M, l;
+  f32x4 o;
+};
+// o += oy, l += ly of a partial result with maximum My
+__device__ __forceinline__ void join_add(JoinSum &s, const float *My, const float *ly, const f32x4 *oy) {
+  float M = s.M;
 #pragma unroll
-    for (int u = 0; u < RT; ++u)
+  for (int i = 0; i < 4; ++i) M = fmaxf(M, My[i]);
+  const float Mu = M == -INFINITY ? 0.0f : M, a0 = __builtin_amdgcn_exp2f(s.M - Mu);
+  s.l *= a0;
+  s.o *= a0;
 #pragma unroll
-      for (int n = 0; n < NT; ++n) sh_o[0][u * NT + n][lane] = acc[u][n];
+  for (int i = 0; i < 4; ++i) {
+    const float al = My[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(My[i] - Mu);
+    s.l = fmaf(ly[i], al, s.l);
+    s.o += oy[i] * al;
+  }
+  s.M = M;
+}
+
+template <int NA, int G, bool DEAL>
+__global__ __launch_bounds__(64 * kJoinWaves) void kv_join_kernel(AttendArgs P, int ru, int spread, float up) {
+  constexpr int W = kJoinWaves, R = 64 / G, F = NA * 256 + 2 * R;  // rows, floats of a block
+  __shared__ float sh[W][R], sl[W][R];
+  __shared__ f32x4 so[W][64];
+  const KvCache &C = P.C;
+  const KvAttend &A = P.A;
+  const uint32_t block = spread ? blockIdx.x / NA : blockIdx.x;
+  uint32_t x = block / (uint32_t)ru;
+  const int u = (int)(block - x * ru);
+  const int64_t tile = x;
+  const int rt = (int)(x % (uint32_t)P.rtiles);
+  x /= (uint32_t)P.rtiles;
+  const int h = (int)(x % (uint32_t)C.heads);
+  const int b = (int)(x / (uint32_t)C.heads);
+  KvSeq q;
+  if (!kv_seq(P.S, C.page, b, &q)) return;
+  const int rows = q.n * A.group, t0 = rt * ru * R, r0 = t0 + u * R;
+  if (r0 >= rows) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % R, g = lane / R;
+  int splits;
+  int64_t first, step;  // block of split 0, blocks from one split to the next
+  int64_t lead = 0;     // split 0 lies this many blocks further
+  if constexpr (DEAL) {
+    const DealScan o = deal_all(P, ru * R);
+    const uint32_t run = (uint32_t)deal_run(P, o.all);
+    KvSeq z;
+    const SeqChunks s = seq_chunks(P, b, ru * R, &z);
+    const uint32_t t = deal_before(P, ru * R, o, b) + (s.n + kTileCost) * (h * (s.tiles / C.heads) + rt) + kTileCost;
+    const uint32_t w0 = t / run, w1 = (t + s.n - 1) / run;
+    splits = (int)(w1 - w0 + 1);
+    first = (int64_t)w0 * 2 * ru + u;
+    step = 2 * ru;
+    lead = ru;
+  } else {
+    int cb, ce;
+    tile_span(P, q, t0, min(t0 + ru * R, rows), 0, &cb, &ce, &splits);
+    first = tile * P.splits * ru + u;
+    step = ru;
+  }
+  if (splits == 1) return;  // already finished
+  const int r = r0 + m;
+  auto sums = [&](int n, int y0, int dy) {  // of splits y0, y0 + dy, ...
+    JoinSum s{-INFINITY, 0.0f, {0, 0, 0, 0}};
+    if (r >= rows) return s;
+    for (; y0 < splits; y0 += 4 * dy) {
+      float My[4], ly[4];
+      f32x4 oy[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // past the last split: the last one again, which does not count
+        const int y = min(y0 + i * dy, splits - 1);
+        const float *p = P.part + (first + y * step + (y == 0 ? lead : 0)) * F;
+        My[i] = y0 + i * dy < splits ? p[NA * 256 + m] : -INFINITY;
+        ly[i] = p[NA * 256 + R + m];
+        oy[i] = *reinterpret_cast<const f32x4 *>(p + (n * 64 + lane) * 4);
+      }
+      join_add(s, My, ly, oy);
+    }
+    return s;
+  };
+  auto finish = [&](int n, const JoinSum &s) {
+    if (r >= rows) return;
+    const RowAt at = row_at(A, C, q, h, r);
+    const f32x4 o = s.o * (s.l == 0.0f ? 0.0f : 1.0f / s.l);
+    const float y[4] = {o.x, o.y, o.z, o.w};
+    const int c = G == 4 ? 16 * n + 4 * g : 32 * (n / 4) + 8 * (n % 4) + 4 * g;
+    if (c < C.d) store_o4(A, at.o + c, y);
+    if (A.lse && n == 0 && g == 0) A.lse[at.lse] = log_sum(s.M, s.l, up);
+  };
+  if (!spread) {
+    for (int n = wave; n < NA; n += W) finish(n, sums(n, 0, 1));
+    return;
+  }
+  const int n = (int)(blockIdx.x - block * NA);
+  JoinSum s = sums(n, wave, W);
+  so[wave][lane] = s.o;
+  if (g == 0) {
+    sh[wave][m] = s.M;
+    sl[wave][m] = s.l;
   }
   __syncthreads();
   if (wave) return;
 #pragma unroll
-  for (int u = 0; u < RT; ++u) {
-    const int r = r0 + 16 * u + m;
-    if (P.splits > 1) {
-      float *o = P.part + ((tile * P.splits + split) * RT + u) * part_floats(NT);
+  for (int y0 = 1; y0 < W; y0 += 4) {
+    float My[4], ly[4];
+    f32x4 oy[4];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        *reinterpret_cast<f32x4 *>(o + (n * 64 + lane) * 4) = acc[u][n] + sh_o[0][u * NT + n][lane];
-      if (g == 0) {
-        o[NT * 256 + m] = M[u];
-        o[NT * 256 + 16 + m] = l[u];
-      }
-      continue;
+    for (int i = 0; i < 4; ++i) {
+      const int y = min(y0 + i, W - 1);
+      My[i] = y0 + i < W ? sh[y][m] : -INFINITY;
+      ly[i] = sl[y][m];
+      oy[i] = so[y][lane];
     }
-    if (r >= rows) continue;
-    const RowAt at = row_at(A, C, q, h, r);
-    const float inv = l[u] == 0.0f ? 0.0f : 1.0f / l[u];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int c = 16 * n + 4 * g;
-      const f32x4 v = (acc[u][n] + sh_o[0][u * NT + n][lane]) * inv;
-      const float y[4] = {v.x, v.y, v.z, v.w};
-      if (c < d) store_o4(A, at.o + c, y);
-    }
-    if (A.lse && g == 0) A.lse[at.lse] = log_sum(M[u], l[u]);
+    join_add(s, My, ly, oy);
   }
-}
-
-// Joins the splits of a tile of 16 rows: one wave per four accumulators of a lane.
-template <int NT>
-__global__ __launch_bounds__(64) void kv_join_kernel(AttendArgs P, int rt16) {
-  const KvCache &C = P.C;
-  const KvAttend &A = P.A;
-  const int n = blockIdx.x % NT;
-  int64_t x = blockIdx.x / NT;
-  const int u = (int)(x % rt16);
-  x /= rt16;
-  const int64_t tile = x;
-  const int rt = (int)(x % P.rtiles);
-  x /= P.rtiles;
-  const int h = (int)(x % C.heads);
-  const int b = (int)(x / C.heads);
-  KvSeq q;
-  if (!kv_seq(P.S, C.page, b, &q)) return;
-  const int rows = q.n * A.group, r0 = (rt * rt16 + u) * 16;
-  if (r0 >= rows) return;
-  const int lane = threadIdx.x, m = lane & 15, g = lane >> 4;
-  const float *base = P.part + (tile * P.splits * rt16 + u) * part_floats(NT);
-  const int64_t step = (int64_t)rt16 * part_floats(NT);
-  float Mx = -INFINITY;
-  for (int y = 0; y < P.splits; ++y) Mx = fmaxf(Mx, base[y * step + NT * 256 + m]);
-  float l = 0.0f;
-  f32x4 o = {0, 0, 0, 0};
-  for (int y = 0; y < P.splits; ++y) {
-    const float *p = base + y * step;
-    const float My = p[NT * 256 + m];
-    if (My == -INFINITY) continue;
-    const float al = __builtin_amdgcn_exp2f(My - Mx);
-    l += p[NT * 256 + 16 + m] * al;
-    o += *reinterpret_cast<const f32x4 *>(p + (n * 64 + lane) * 4) * al;
-  }
-  const int r = r0 + m;
-  if (r >= rows) return;
-  const RowAt at = row_at(A, C, q, h, r);
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  o *= inv;
-  const float y[4] = {o.x, o.y, o.z, o.w};
-  const int c = 16 * n + 4 * g;
-  if (c < C.d) store_o4(A, at.o + c, y);
-  if (A.lse && n == 0 && g == 0) A.lse[at.lse] = log_sum(Mx, l);
+  finish(n, s);
 }
 
 // ---- many rows: tiles of 64 positions shared by a workgroup through LDS ------------------------------------------------
@@ -469,6 +718,8 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   if (!kv_seq(P.S, C.page, b, &q)) return;
   const int rows = q.n * A.group, r0 = rt * 32 * RC * kWaves;
   if (r0 >= rows) return;
+  int cb, ce, splits;
+  if (!tile_span(P, q, r0, min(r0 + 32 * RC * kWaves, rows), split, &cb, &ce, &splits)) return;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, m = lane & 31, g = lane >> 5;
   const int d = C.d;
   const int rw = r0 + 32 * RC * wave;  // this wave's first row
@@ -480,36 +731,28 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   for (int u = 0; u < RC; ++u) {
     const int r = min(rw + 32 * u + m, rows - 1);
     row_span(A, q, r, &lo[u], &hi[u]);
-    const int64_t at = row_at(A, C, q, h, r).q;
-    float top = 0.0f;
-    float v[2 * ND][8];
+    const uint16_t *at = static_cast<const uint16_t *>(A.q.p) + row_at(A, C, q, h, r).q;
+    u32x4 raw[ND][2];  // pairs of 8 values: dims 32 n + 8 g and 16 further
 #pragma unroll
-    for (int k = 0; k < 2 * ND; ++k) {
-      const int c = 16 * k + 8 * g;
-      if (c < d) {
-        if (A.type == KM_T_BF16) kv_load<KM_T_BF16, 8>(A.q.p, at + c, v[k]);
-        else kv_load<KM_T_F16, 8>(A.q.p, at + c, v[k]);
-      } else {
+    for (int n = 0; n < ND; ++n)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
-      }
+      for (int i = 0; i < 2; ++i)
+        raw[n][i] = *reinterpret_cast<const u32x4 *>(at + min(32 * n + 16 * i, d - 16) + 8 * g);
+    float top = 0.0f, f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[k][i]));
-    }
-    float f;
+    for (int n = 0; n < ND; ++n) top = fmaxf(top, top16<1>(raw[n], A.type));
     q_scale(max_halves(top), A.scale, &f, &cs[u]);
 #pragma unroll
-    for (int k = 0; k < 2 * ND; ++k)
+    for (int n = 0; n < ND; ++n) {
+      float v[16];
+      values16<1>(raw[n], A.type, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) qf[u][k][i] = (_Float16)(v[k][i] * f);
+      for (int i = 0; i < 16; ++i)
+        qf[u][2 * n + i / 8][i % 8] = 32 * n + 16 * (i / 8) < d ? (_Float16)(v[i] * f) : (_Float16)0.0f;
+    }
   }
-  // tiles of the workgroup's rows, and of this wave's
+  // the tiles of this wave's rows
   int jlo, jhi, any;
-  row_span(A, q, r0, &jlo, &any);
-  row_span(A, q, min(r0 + 32 * RC * kWaves, rows) - 1, &any, &jhi);
-  const int c0 = jlo / kChunk, c1 = jhi > jlo ? (int)cdiv(jhi, kChunk) : c0;
-  const int per = (c1 - c0 + P.splits - 1) / P.splits;
-  const int cb = c0 + split * per, ce = min(cb + per, c1);
   row_span(A, q, min(rw, rows - 1), &jlo, &any);
   row_span(A, q, min(rw + 32 * RC, rows) - 1, &any, &jhi);
   const int wb = max(cb, jlo / kChunk), we = rw < rows ? min(ce, (int)cdiv(jhi, kChunk)) : cb;
@@ -599,9 +842,9 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   // codes past the end may be NaN, which no weight of 0 takes out
   auto clear_values = [&](int c) {
     if constexpr (FMT == KM_KV_F8) {
-      const int left = rthere ? q.len - c * kChunk - 16 * run : 0;
+      int left = rthere ? q.len - c * kChunk - 16 * run : 0;
       if (left < 16) {
-        asm volatile("");  // a branch: rarely taken
+        asm volatile("" : "+v"(left));  // a branch: rarely taken
 #pragma unroll
         for (int i = 0; i < VP; ++i)
 #pragma unroll
@@ -691,12 +934,13 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
 #pragma unroll
       for (int u = 0; u < RC; ++u) {
         if (!__all(there && j0 >= lo[u] && j0 + kChunk <= hi[u])) {
-          asm volatile("");  // a branch: few tiles need it
+          int jg = j0 + 8 * g;
+          asm volatile("" : "+v"(jg));  // a branch: few tiles need it, so nothing of it is kept in registers
 #pragma unroll
           for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const int j = j0 + 32 * tt + 16 * (i >> 3) + 8 * g + (i & 7);
+              const int j = jg + 32 * tt + 16 * (i >> 3) + (i & 7);
               if (j < lo[u] || j >= hi[u] || sc[c & 1][ONE ? 0 : 2 * tt + (i >> 3)].w == 0.0f) s[tt][u][i] = -INFINITY;
             }
         }
@@ -803,11 +1047,10 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   for (int u = 0; u < RC; ++u) {
     l[u] += __shfl_xor(l[u], 32);
     const int r = rw + 32 * u + m;
-    if (P.splits > 1) {
-      if (rw + 32 * u >= rows) return;
+    if (splits > 1) {
+      if (r >= rows) continue;
       if (l[u] != l[u]) M[u] = INFINITY;  // the maximum does not see NaN
-      const int64_t tile = ((bh * P.rtiles + rt) * kWaves + wave) * RC + u;
-      float *o = P.part + (tile * P.splits + split) * part32_floats(ND);
+      float *o = P.part + ((((bh * P.rtiles + rt) * P.splits + split) * kWaves + wave) * RC + u) * part32_floats(ND);
 #pragma unroll
       for (int n = 0; n < ND; ++n)
 #pragma unroll
@@ -836,49 +1079,10 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   }
 }
 
-// Joins the splits of 32 rows: a wave per four accumulators of a lane.
-template <int ND>
-__global__ __launch_bounds__(64) void kv_prompt_join_kernel(AttendArgs P, int W) {
-  const KvCache &C = P.C;
-  const KvAttend &A = P.A;
-  const int n = blockIdx.x % (4 * ND);
-  const int64_t tile = blockIdx.x / (4 * ND);
-  int64_t x = tile / W;
-  const int rt = (int)(x % P.rtiles);
-  x /= P.rtiles;
-  const int h = (int)(x % C.heads);
-  const int b = (int)(x / C.heads);
-  KvSeq q;
-  if (!kv_seq(P.S, C.page, b, &q)) return;
-  const int rows = q.n * A.group, r0 = (rt * W + (int)(tile % W)) * 32;
-  if (r0 >= rows) return;
-  const int lane = threadIdx.x, m = lane & 31, g = lane >> 5;
-  const float *base = P.part + tile * P.splits * part32_floats(ND);
-  float Mx = -INFINITY;
-  for (int y = 0; y < P.splits; ++y) Mx = fmaxf(Mx, base[(int64_t)y * part32_floats(ND) + ND * 1024 + m]);
-  float l = 0.0f;
-  f32x4 o = {0, 0, 0, 0};
-  for (int y = 0; y < P.splits; ++y) {
-    const float *p = base + (int64_t)y * part32_floats(ND);
-    const float My = p[ND * 1024 + m];
-    if (My == -INFINITY) continue;
-    const float al = __builtin_amdgcn_exp2f(My - Mx);
-    l += p[ND * 1024 + 32 + m] * al;
-    o += *reinterpret_cast<const f32x4 *>(p + (n * 64 + lane) * 4) * al;
-  }
-  const int r = r0 + m;
-  if (r >= rows) return;
-  const RowAt at = row_at(A, C, q, h, r);
-  o *= l == 0.0f ? 0.0f : 1.0f / l;
-  const float y[4] = {o.x, o.y, o.z, o.w};
-  const int c = 32 * (n / 4) + 8 * (n % 4) + 4 * g;
-  if (c < C.d) store_o4(A, at.o + c, y);
-  if (A.lse && n == 0 && g == 0) A.lse[at.lse] = log_sum(Mx, l, kUp32);
-}
-
 struct Plan {
   bool prompt;
-  int nt, rt, rtiles, splits;
+  int nt, rt, rtiles, deal, splits, per;
+  int spread;  // the join has a workgroup per accumulator of a lane
   int64_t tiles;
 };
 
@@ -896,47 +1100,64 @@ int dim_tiles32(int d) {
 constexpr int row_tiles(int nd) { return 1; }
 
 Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
-  Plan p;
+  Plan p{};
   const int64_t rows = (int64_t)S.max_rows * A.group;
-  const int64_t len = A.window ? std::min<int64_t>(S.max_len, (int64_t)A.window + S.max_rows) : S.max_len;
+  // the most chunks that a tile's rows see
+  const int64_t len = A.window ? std::min<int64_t>(S.max_len, (int64_t)A.window + S.max_rows + kChunk) : S.max_len;
+  const int64_t chunks = std::max<int64_t>(1, cdiv(len, kChunk));
   p.prompt = rows > 32 && A.type != KM_T_F32;
-  if (p.prompt) {
-    p.nt = dim_tiles32(C.d);
-    p.rt = kWaves * row_tiles(p.nt);
-    p.rtiles = (int)cdiv(rows, 32 * p.rt);
-    p.tiles = (int64_t)S.n * C.heads * p.rtiles;
-    const int64_t most = std::max<int64_t>(1, len / (8 * kChunk));
-    p.splits = (int)std::min(most, std::max<int64_t>(1, 512 / p.tiles));
-    return p;
-  }
-  p.nt = dim_tiles(C.d);
-  p.rt = rows > 16 && A.type != KM_T_F32 ? 2 : 1;
-  p.rtiles = (int)cdiv(rows, 16 * p.rt);
+  p.nt = p.prompt ? dim_tiles32(C.d) : dim_tiles(C.d);
+  p.rt = p.prompt ? kWaves * row_tiles(p.nt) : rows > 16 && A.type != KM_T_F32 && p.nt <= 8 ? 2 : 1;
+  p.rtiles = (int)cdiv(rows, (p.prompt ? 32 : 16) * p.rt);
   p.tiles = (int64_t)S.n * C.heads * p.rtiles;
-  // enough workgroups for every CU to hold two; a split of fewer than four chunks leaves waves without work
-  const int64_t most = std::max<int64_t>(1, cdiv(len, 4 * kChunk));
-  p.splits = (int)std::min(most, std::max<int64_t>(1, 512 / p.tiles));
+  if (p.prompt) {
+    p.per = (int)std::max<int64_t>(8, cdiv(p.tiles * chunks, 512));
+    p.spread = p.tiles * p.rt < 256;
+  } else {
+    // Short contexts, or rows enough that tiles fill the card several times: a workgroup for each tile and no join.  A
+    // workgroup takes 6.5 us and 1.7 more per 256 positions (8 heads of 128); splitting it up and joining takes 14 us whatever
+    // the length.  Where that leaves every workgroup little to do, even splits; where it streams for long, what
+    // differing lengths leave idle counts for more, and tiles are dealt out (64 sequences of 1 to 16384 tokens: 194 us, even
+    // splits 225; 16 sequences behind a window of 4096: 39 us, even splits 28).  As many workgroups as run at a time.
+    const int64_t cap = (int64_t)S.max_pages * C.page / kChunk + 1 + kTileCost;  // whatever max_len says
+    const int64_t most = p.nt <= 8 ? 512 : 256;
+    p.spread = p.tiles * p.rt < 256;
+    if (p.rtiles > 4 || chunks <= (p.tiles < 256 ? 16 : 32)) {
+      p.per = (int)chunks;
+    } else if (p.tiles * chunks <= 16 * most || S.n == 1 || p.tiles * cap >= INT32_MAX) {
+      p.per = (int)std::max<int64_t>(kAttendWaves, cdiv(p.tiles * chunks, most));
+    } else {
+      p.deal = 1;
+      p.per = 2 * kAttendWaves;
+      p.splits = (int)std::min<int64_t>(most, cdiv(p.tiles * chunks, p.per));
+      return p;
+    }
+  }
+  p.splits = (int)cdiv(chunks, p.per);
   return p;
 }
 
 }  // namespace
 
+static int accumulators(const Plan &p) { return p.nt * (p.prompt ? 4 : 1); }
+static int64_t join_blocks(const Plan &p) { return p.tiles * p.rt * (p.spread ? accumulators(p) : 1); }
+
 int64_t kv_attend_blocks(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   const Plan p = plan(C, S, A);
-  return p.tiles * std::max(p.splits, p.rt * p.nt * (p.prompt ? 4 : 1));  // the join's grid is the larger one
+  return std::max(p.tiles * (p.deal ? 1 : p.splits), join_blocks(p));
 }
 
 size_t kv_attend_scratch(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   const Plan p = plan(C, S, A);
-  return p.splits > 1 ? sizeof(float) * (size_t)p.tiles * p.splits * p.rt *
-                            (p.prompt ? part32_floats(p.nt) : part_floats(p.nt))
-                      : 0;
+  if (p.splits == 1 && !p.deal) return 0;
+  return sizeof(float) * (size_t)(p.deal ? 2 : p.tiles) * p.splits * p.rt *
+         (p.prompt ? part32_floats(p.nt) : part_floats(p.nt));
 }
 
 km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A, void *ws, hipStream_t s) {
   const Plan p = plan(C, S, A);
-  AttendArgs P{C, S, A, p.rtiles, p.splits, static_cast<float *>(ws)};
-  const dim3 grid((unsigned)(p.tiles * p.splits));
+  AttendArgs P{C, S, A, p.rtiles, p.deal, p.splits, p.per, static_cast<float *>(ws)};
+  const dim3 grid((unsigned)(p.deal ? p.splits : p.tiles * p.splits));
   if (p.prompt) {
 #define KV_K(F, N)                                                                         \
   C.page >= kChunk ? kv_prompt_kernel<F, N, row_tiles(N), true><<<grid, 64 * kWaves, 0, s>>>(P) \
@@ -947,7 +1168,7 @@ km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A,
     else KV_K(KM_KV_F8, N);                                                                                     \
     KMQ_LAUNCH_CHECK("kv_attend");                                                                              \
     if (p.splits > 1)                                                                                           \
-      kv_prompt_join_kernel<N><<<dim3((unsigned)(p.tiles * p.rt * 4 * N)), 64, 0, s>>>(P, p.rt);                \
+      kv_join_kernel<4 * N, 2, false><<<dim3((unsigned)join_blocks(p)), 64 * kJoinWaves, 0, s>>>(P, p.rt, p.spread, kUp32);        \
     break;
     switch (p.nt) {
       KV_N(2)
@@ -961,10 +1182,12 @@ km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A,
     KMQ_LAUNCH_CHECK("kv_attend");
     return KM_OK;
   }
-#define KV_K(F, N, R, Z) kv_attend_kernel<F, N, R, Z><<<grid, 256, 0, s>>>(P)
+#define KV_K(F, N, R, Z)                                                              \
+  C.page >= kChunk ? kv_attend_kernel<F, N, R, Z, true><<<grid, 64 * kAttendWaves, 0, s>>>(P) \
+                   : kv_attend_kernel<F, N, R, Z, false><<<grid, 64 * kAttendWaves, 0, s>>>(P)
 #define KV_R(F, N)                          \
   if (A.type == KM_T_F32) KV_K(F, N, 1, 2); \
-  else if (p.rt == 2) KV_K(F, N, 2, 1);     \
+  else if (p.rt == 2) KV_K(F, N, (N <= 8 ? 2 : 1), 1); \
   else KV_K(F, N, 1, 1);
 #define KV_N(N)                                                                                         \
   case N:                                                                                               \
@@ -974,7 +1197,10 @@ km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A,
       KV_R(KM_KV_F8, N)                                                                                 \
     }                                                                                                   \
     KMQ_LAUNCH_CHECK("kv_attend");                                                                      \
-    if (p.splits > 1) kv_join_kernel<N><<<dim3((unsigned)(p.tiles * p.rt * N)), 64, 0, s>>>(P, p.rt);   \
+    if (p.deal)                                                                                         \
+      kv_join_kernel<N, 4, true><<<dim3((unsigned)join_blocks(p)), 64 * kJoinWaves, 0, s>>>(P, p.rt, p.spread, kUp); \
+    else if (p.splits > 1)                                                                              \
+      kv_join_kernel<N, 4, false><<<dim3((unsigned)join_blocks(p)), 64 * kJoinWaves, 0, s>>>(P, p.rt, p.spread, kUp);          \
     break;
   switch (p.nt) {
     KV_N(4)
