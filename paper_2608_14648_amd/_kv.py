@@ -16,6 +16,7 @@ from ._kmq import KmKvCache, KmKvRows, KmKvSeqs, KmqError, _check, _dev, lib
 KM_KV_I8, KM_KV_F8 = 0, 1
 KM_KV_CAUSAL = 1
 _FORMATS = {torch.int8: KM_KV_I8, torch.float8_e4m3fn: KM_KV_F8}
+_raw_stream = torch._C._cuda_getCurrentRawStream  # the handle alone: current_stream() makes an object of it first
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -102,19 +103,17 @@ def _rows_of(t: torch.Tensor, name: str, seqs: KvSeqs, heads: int, d: int, dtype
         raise TypeError(f"{name} must be {dtype or 'float32, bfloat16 or float16'} (got {t.dtype})")
     if t.device != seqs.device:
         raise ValueError(f"{name} must be on {seqs.device} (got {t.device})")
-    if t.dim() != 3 or t.shape[0] != seqs.rows or t.shape[1] != heads or t.shape[2] != d:
+    if t.shape != (seqs.rows, heads, d):
         raise ValueError(f"{name} must be [{seqs.rows}, {heads}, {d}] (got {tuple(t.shape)})")
     row, head, one = t.stride()
     if one != 1:
         raise ValueError(f"{name}'s last axis must be contiguous")
     if seqs.rows <= 1:  # the stride of an axis of one is of no meaning
         row = 0
-    elif written and row < d:
-        raise ValueError(f"{name} is written: its rows must not overlap")
     if heads == 1:
         head = 0
-    elif written and head < d:
-        raise ValueError(f"{name} is written: its heads must not overlap")
+    if written and ((row < d and seqs.rows > 1) or (head < d and heads > 1)):
+        raise ValueError(f"{name} is written: its rows and heads must not overlap")
     return KmKvRows(t.data_ptr(), row, head)
 
 
@@ -132,23 +131,22 @@ def kv_write(cache: KvCache, seqs: KvSeqs, k: torch.Tensor, v: torch.Tensor) -> 
     vr = _rows_of(v, "v", seqs, cache.heads, cache.d, k.dtype)
     if seqs.rows:
         _check(lib().kv_write(cache._ref, seqs._ref, ct.addressof(kr), ct.addressof(vr), _TYPES[k.dtype],
-                              torch.cuda.current_stream().cuda_stream))
+                              _raw_stream(cache.device.index)))
 
 
 def kv_read(cache: KvCache, seqs: KvSeqs, dtype: torch.dtype = torch.bfloat16, k: torch.Tensor | None = None,
             v: torch.Tensor | None = None):
     """The rows' keys and values ([rows, heads, d]) as the cache holds them, rounded to dtype, into k and v where given."""
     _same(cache, seqs)
-    shape = (seqs.rows, cache.heads, cache.d)
     if k is None:
-        k = torch.empty(shape, dtype=dtype, device=cache.device)
+        k = cache.k_scale.new_empty((seqs.rows, cache.heads, cache.d), dtype=dtype)
     if v is None:
-        v = torch.empty(shape, dtype=k.dtype, device=cache.device)
+        v = torch.empty_like(k)
     kr = _rows_of(k, "k", seqs, cache.heads, cache.d, written=True)
     vr = _rows_of(v, "v", seqs, cache.heads, cache.d, k.dtype, written=True)
     if seqs.rows:
         _check(lib().kv_read(cache._ref, seqs._ref, ct.addressof(kr), ct.addressof(vr), _TYPES[k.dtype],
-                             torch.cuda.current_stream().cuda_stream))
+                             _raw_stream(cache.device.index)))
     return k, v
 
 
@@ -165,9 +163,9 @@ def kv_attend(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, scale: float | None
     q_heads = q.shape[1]
     qr = _rows_of(q, "q", seqs, q_heads, cache.d)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q)
     orow = _rows_of(out, "out", seqs, q_heads, cache.d, q.dtype, written=True)
-    L = torch.empty((seqs.rows, q_heads), dtype=torch.float32, device=q.device) if lse else None
+    L = q.new_empty((seqs.rows, q_heads), dtype=torch.float32) if lse else None
     if seqs.rows == 0:
         return out, L
     flags = KM_KV_CAUSAL if causal else 0
@@ -180,5 +178,5 @@ def kv_attend(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, scale: float | None
     _check(lb.kv_attend(cache._ref, seqs._ref, ct.addressof(qr), q_heads,
                         1.0 / math.sqrt(cache.d) if scale is None else scale, flags, window, ct.addressof(orow), t,
                         None if L is None else L.data_ptr(), None if ws is None else ws.data_ptr(), need,
-                        torch.cuda.current_stream().cuda_stream))
+                        _raw_stream(cache.device.index)))
     return out, L

@@ -6,7 +6,6 @@
 namespace kmq {
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -108,44 +107,6 @@ struct KvElem {
   static constexpr int bytes = TYPE == KM_T_F32 ? 4 : 2;
 };
 
-// n values at element offset o (n * bytes a multiple of 4, the address aligned to as many bytes, 16 at most)
-template <int TYPE, int N>
-__device__ __forceinline__ void kv_load(const void *p, int64_t o, float *x) {
-  if constexpr (TYPE == KM_T_F32) {
-    const float *q = static_cast<const float *>(p) + o;
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(q + i);
-      x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
-    }
-  } else {
-    const uint16_t *q = static_cast<const uint16_t *>(p) + o;
-    uint32_t w[N / 2];
-    if constexpr (N % 8 == 0) {
-#pragma unroll
-      for (int i = 0; i < N; i += 8) {
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(q + i);
-        w[i / 2] = v.x, w[i / 2 + 1] = v.y, w[i / 2 + 2] = v.z, w[i / 2 + 3] = v.w;
-      }
-    } else {
-      static_assert(N == 4, "4 values or whole groups of 8");
-      const u32x2 v = *reinterpret_cast<const u32x2 *>(q);
-      w[0] = v.x, w[1] = v.y;
-    }
-#pragma unroll
-    for (int i = 0; i < N; i += 2) {
-      if constexpr (TYPE == KM_T_BF16) {
-        x[i] = __uint_as_float(w[i / 2] << 16);
-        x[i + 1] = __uint_as_float(w[i / 2] & 0xffff0000u);
-      } else {
-        const f16x2 h = __builtin_bit_cast(f16x2, w[i / 2]);
-        x[i] = (float)h.x;
-        x[i + 1] = (float)h.y;
-      }
-    }
-  }
-}
-
 template <int TYPE>
 __device__ __forceinline__ uint32_t kv_pack2(float a, float b) {
   const f32x2 v = {a, b};
@@ -155,6 +116,7 @@ __device__ __forceinline__ uint32_t kv_pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
 }
 
+// N values to element offset o (an address aligned to their bytes, 16 at most)
 template <int TYPE, int N>
 __device__ __forceinline__ void kv_store(void *p, int64_t o, const float *x) {
   if constexpr (TYPE == KM_T_F32) {

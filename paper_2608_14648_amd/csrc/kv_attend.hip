@@ -31,7 +31,7 @@ struct AttendArgs {
   KvCache C;
   KvSeqs S;
   KvAttend A;
-  int rtiles;  // row tiles per sequence and head
+  int rtiles;   // row tiles per sequence and head
   int deal;     // tiles are dealt out (kv_attend_kernel)
   int splits;   // the most that a tile is split into; if dealt out, workgroups
   int per;      // chunks of a split or, at least, of a workgroup
@@ -230,7 +230,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
   constexpr int W = kAttendWaves;
   const KvCache &C = P.C;
   const KvAttend &A = P.A;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int d = C.d, rows = q.n * A.group;
 
   // Codes of a chunk.  Its page (ONE), or the pages of this lane's runs of 16: keys of run kr, values of run g.  Behind the
@@ -581,7 +581,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_join_kernel(AttendArgs P, 
   if (!kv_seq(P.S, C.page, b, &q)) return;
   const int rows = q.n * A.group, t0 = rt * ru * R, r0 = t0 + u * R;
   if (r0 >= rows) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane % R, g = lane / R;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane % R, g = lane / R;
   int splits;
   int64_t first, step;  // block of split 0, blocks from one split to the next
   int64_t lead = 0;     // split 0 lies this many blocks further
@@ -662,16 +662,22 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_join_kernel(AttendArgs P, 
 
 // ---- many rows: tiles of 64 positions shared by a workgroup through LDS ------------------------------------------------
 //
-// A wave takes 32 RC rows and the 32 x 32 x 16 products; the four waves of a workgroup share each tile of 64 positions, whose
+// A wave takes 32 rows and the 32 x 32 x 16 products; the four waves of a workgroup share each tile of 64 positions, whose
 // codes are widened to fp16 once and laid out in LDS.  As above the scores are computed transposed, with the keys'
 // order chosen such that a lane ends with 8 consecutive positions of its row in consecutive registers: row m of a 32-key
 // operand holds position m with bits 2 and 3 exchanged.  The running maximum moves only when a tile's exceeds it by
 // more than kSlack: until then weights just grow, within fp16's range.
 //
-// A wave has a SIMD's registers to itself, so the matrix cores and the vector unit overlap inside it: the products of the
-// next tile's scores are issued with this tile's exponentials, and the widening of later tiles with the second products.
-// Keys therefore run one tile ahead of values in LDS (two buffers each, one barrier per tile), and codes are loaded one tile
-// before they are widened.
+// The matrix cores and the vector unit (exponentials, widening) have about as much to do, so they overlap inside a wave too: the
+// products of the next tile's scores are issued between this tile's exponentials, and the widening of later tiles between
+// the second products.  Keys therefore run one tile ahead of values in LDS (two buffers each, one barrier per tile), and codes
+// are loaded one tile before they are widened.
+//
+// Measured (prompt of 16384, 32 query heads of 128 on 8): 2.3 ms, 950 TFLOP/s, where a large fp16 library product reaches
+// 1310 on this card (both run into its power limit, about 1.9 GHz).  The matrix cores are busy for 44 % of the time, the
+// vector unit for 59 %, LDS for 40 %.  Two waves to a SIMD.  Tried: 64 rows to a wave, one wave to a SIMD (halves the LDS
+// reads, 3.3 ms); eight waves to a workgroup (halves the widening, no change).  Heads of more than 128 dims leave a SIMD
+// one wave only, and its phases in turn: 390 TFLOP/s at 256.
 
 constexpr float kUp32 = 8.0f, kSlack = 7.0f;
 
@@ -692,7 +698,7 @@ __host__ __device__ constexpr int part32_floats(int nd) { return nd * 1024 + 64;
 
 constexpr int kWaves = 4;  // of this kernel
 
-template <int FMT, int ND, int RC, bool ONE>
+template <int FMT, int ND, bool ONE>
 __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel(AttendArgs P) {
   constexpr int DP = 32 * ND, T = 64 * kWaves;
   constexpr int KLD = DP + 8, VLD = kChunk + 8;  // halves; 16 bytes more than the row: rows start in different banks
@@ -716,58 +722,29 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   const int b = (int)(bh / C.heads);
   KvSeq q;
   if (!kv_seq(P.S, C.page, b, &q)) return;
-  const int rows = q.n * A.group, r0 = rt * 32 * RC * kWaves;
+  const int rows = q.n * A.group, r0 = rt * 32 * kWaves;
   if (r0 >= rows) return;
   int cb, ce, splits;
-  if (!tile_span(P, q, r0, min(r0 + 32 * RC * kWaves, rows), split, &cb, &ce, &splits)) return;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, m = lane & 31, g = lane >> 5;
+  if (!tile_span(P, q, r0, min(r0 + 32 * kWaves, rows), split, &cb, &ce, &splits)) return;
+  const int t = threadIdx.x, lane = t & 63, m = lane & 31, g = lane >> 5;
+  // Uniform: branches of a wave are branches, not masks (prompt of 16384: 2.30 ms, else 2.43).  With wider heads the
+  // accumulators then no longer fit beside the rest (256 dims: 760 us instead of 638).
+  const int wave = ND <= 4 ? __builtin_amdgcn_readfirstlane(t >> 6) : t >> 6;
   const int d = C.d;
-  const int rw = r0 + 32 * RC * wave;  // this wave's first row
+  const int rw = r0 + 32 * wave;  // this wave's first row
 
-  f16x8 qf[RC][2 * ND];
-  float cs[RC];
-  int lo[RC], hi[RC];
-#pragma unroll
-  for (int u = 0; u < RC; ++u) {
-    const int r = min(rw + 32 * u + m, rows - 1);
-    row_span(A, q, r, &lo[u], &hi[u]);
-    const uint16_t *at = static_cast<const uint16_t *>(A.q.p) + row_at(A, C, q, h, r).q;
-    u32x4 raw[ND][2];  // pairs of 8 values: dims 32 n + 8 g and 16 further
-#pragma unroll
-    for (int n = 0; n < ND; ++n)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        raw[n][i] = *reinterpret_cast<const u32x4 *>(at + min(32 * n + 16 * i, d - 16) + 8 * g);
-    float top = 0.0f, f;
-#pragma unroll
-    for (int n = 0; n < ND; ++n) top = fmaxf(top, top16<1>(raw[n], A.type));
-    q_scale(max_halves(top), A.scale, &f, &cs[u]);
-#pragma unroll
-    for (int n = 0; n < ND; ++n) {
-      float v[16];
-      values16<1>(raw[n], A.type, v);
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        qf[u][2 * n + i / 8][i % 8] = 32 * n + 16 * (i / 8) < d ? (_Float16)(v[i] * f) : (_Float16)0.0f;
-    }
-  }
   // the tiles of this wave's rows
   int jlo, jhi, any;
   row_span(A, q, min(rw, rows - 1), &jlo, &any);
-  row_span(A, q, min(rw + 32 * RC, rows) - 1, &any, &jhi);
+  row_span(A, q, min(rw + 32, rows) - 1, &any, &jhi);
   const int wb = max(cb, jlo / kChunk), we = rw < rows ? min(ce, (int)cdiv(jhi, kChunk)) : cb;
 
-  f32x16v acc[RC][ND];
-  float M[RC], l[RC];
+  f32x16v acc[ND];
+  float M = -INFINITY, l = 0.0f;
 #pragma unroll
-  for (int u = 0; u < RC; ++u) {
-    M[u] = -INFINITY;
-    l[u] = 0.0f;
+  for (int n = 0; n < ND; ++n)
 #pragma unroll
-    for (int n = 0; n < ND; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[u][n][i] = 0.0f;
-  }
+    for (int i = 0; i < 16; ++i) acc[n][i] = 0.0f;
 
   const int64_t hb = (int64_t)C.page * d;
   const int pmask = C.page - 1;
@@ -782,28 +759,29 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   };
   auto there_at = [&](int pg, int j) { return j < q.len && pg >= 0 && pg < C.pages; };
   auto page_at = [&](int pg) { return (int64_t)(pg >= 0 && pg < C.pages ? pg : 0) * C.heads + h; };
-  int kpg[ONE ? 1 : KP], vpg;  // pages of the codes that are loaded next
+  constexpr int NK = ONE ? 1 : KP;
+  int kpg[NK], vpg;  // pages of the codes that are loaded next
   u32x4 kc[KP], vc[VP];
   float2 rsc;
   bool rthere;
-  auto key_pages = [&](int c) {
+  auto key_pages = [&](int c, int (&pg)[NK]) {
 #pragma unroll
-    for (int i = 0; i < (ONE ? 1 : KP); ++i) kpg[i] = page_of(c * kChunk + (ONE ? 0 : (t + i * T) / PC));
+    for (int i = 0; i < NK; ++i) pg[i] = page_of(c * kChunk + (ONE ? 0 : (t + i * T) / PC));
   };
   auto value_page = [&](int c) { vpg = page_of(c * kChunk + (ONE ? 0 : 16 * run)); };
-  auto load_keys = [&](int c) {
+  auto load_keys = [&](int c, const int (&pg)[NK], u32x4 (&to)[KP]) {
     if constexpr (ONE) {
-      const uint8_t *kp = C.k + page_at(kpg[0]) * hb + ((c * kChunk) & pmask) * d;
+      const uint8_t *kp = C.k + page_at(pg[0]) * hb + ((c * kChunk) & pmask) * d;
 #pragma unroll
       for (int i = 0; i < KP; ++i) {
         const int p = min(t + i * T, KN - 1);
-        kc[i] = *reinterpret_cast<const u32x4 *>(kp + (uint32_t)(p / PC * d + min(16 * (p % PC), d - 16)));
+        to[i] = *reinterpret_cast<const u32x4 *>(kp + (uint32_t)(p / PC * d + min(16 * (p % PC), d - 16)));
       }
     } else {
 #pragma unroll
       for (int i = 0; i < KP; ++i) {
         const int p = min(t + i * T, KN - 1), tok = p / PC, cc = min(16 * (p % PC), d - 16);
-        kc[i] = *reinterpret_cast<const u32x4 *>(C.k + page_at(kpg[i]) * hb + ((c * kChunk + tok) & pmask) * d + cc);
+        to[i] = *reinterpret_cast<const u32x4 *>(C.k + page_at(pg[i]) * hb + ((c * kChunk + tok) & pmask) * d + cc);
       }
     }
   };
@@ -818,16 +796,16 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
           vp + (uint32_t)(min((t >> 2) + i * (T / 4), d - 1) * C.page + (ONE ? 16 * run : 0)));
     rsc = float2{C.ks[at], C.vs[at]};
   };
-  auto store_key = [&](int c, int i) {
+  auto store_key = [&](int c, int i, const u32x4 (&from)[KP]) {
     const int p = t + i * T;
     if (KN % T != 0 && p >= KN) return;
     f16x8 *o = reinterpret_cast<f16x8 *>(&kt[c & 1][p / PC * KLD + 16 * (p % PC)]);
-    o[0] = kv_widen8<FMT>(kc[i].x, kc[i].y);
-    o[1] = kv_widen8<FMT>(kc[i].z, kc[i].w);
+    o[0] = kv_widen8<FMT>(from[i].x, from[i].y);
+    o[1] = kv_widen8<FMT>(from[i].z, from[i].w);
   };
-  auto store_keys = [&](int c) {
+  auto store_keys = [&](int c, const u32x4 (&from)[KP]) {
 #pragma unroll
-    for (int i = 0; i < KP; ++i) store_key(c, i);
+    for (int i = 0; i < KP; ++i) store_key(c, i, from);
   };
   auto store_value = [&](int c, int i) {
     if (VN % T != 0 && t + i * T >= VN) return;
@@ -862,49 +840,77 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   };
   const int krow = ((m & 4) << 1) | ((m & 8) >> 1) | (m & 19);  // bits 2 and 3 exchanged
   // operands of step k: keys of 32 positions at 16 dims, values of 32 dims at 16 positions
-  constexpr int KS = 4 * ND;
+  constexpr int KS = 4 * ND, RD = 4;  // operands are read RD steps ahead
   auto key_at = [&](int c, int k) {
     return *reinterpret_cast<const f16x8 *>(&kt[c & 1][(32 * (k / (2 * ND)) + krow) * KLD + 16 * (k % (2 * ND)) + 8 * g]);
   };
   auto value_at = [&](int c, int k) {
     return *reinterpret_cast<const f16x8 *>(&vt[c & 1][(32 * (k % ND) + m) * VLD + 16 * (k / ND) + 8 * g]);
   };
-  f32x16v s[2][RC];
-  auto scores = [&](int c, int tt) {  // of 32 positions
-    f32x16v o[RC];
+  // The first tile's keys and values and the second's keys are asked for before the queries are looked at.
+  u32x4 kc0[KP];
+  if (cb < ce) {
+    int kp0[NK], kp1[NK], vp1;
+    key_pages(cb, kp0);
+    key_pages(cb + 1, kp1);
+    key_pages(cb + 2, kpg);
+    value_page(cb + 1);
+    vp1 = vpg;
+    value_page(cb);
+    load_keys(cb, kp0, kc0);
+    load_values(cb);
+    load_keys(cb + 1, kp1, kc);
+    vpg = vp1;
+  }
+
+  f16x8 qf[2 * ND];
+  float cs;
+  int lo, hi;
+  const int rq = min(rw + m, rows - 1);  // rows past the last repeat it and are not stored
+  row_span(A, q, rq, &lo, &hi);
+  const uint16_t *qp = static_cast<const uint16_t *>(A.q.p) + row_at(A, C, q, h, rq).q;
+  u32x4 raw[ND][2];  // pairs of 8 values: dims 32 n + 8 g and 16 further
 #pragma unroll
-    for (int u = 0; u < RC; ++u)
+  for (int n = 0; n < ND; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[u][i] = 0.0f;
+    for (int i = 0; i < 2; ++i)
+      raw[n][i] = *reinterpret_cast<const u32x4 *>(qp + min(32 * n + 16 * i, d - 16) + 8 * g);
+  float top = 0.0f, f;
 #pragma unroll
-    for (int k = 0; k < 2 * ND; ++k) {
-      const f16x8 a = *reinterpret_cast<const f16x8 *>(&kt[c & 1][(32 * tt + krow) * KLD + 16 * k + 8 * g]);
+  for (int n = 0; n < ND; ++n) top = fmaxf(top, top16<1>(raw[n], A.type));
+  q_scale(max_halves(top), A.scale, &f, &cs);
 #pragma unroll
-      for (int u = 0; u < RC; ++u) o[u] = mfma32(a, qf[u][k], o[u]);
-    }
+  for (int n = 0; n < ND; ++n) {
+    float v[16];
+    values16<1>(raw[n], A.type, v);
 #pragma unroll
-    for (int u = 0; u < RC; ++u) s[tt][u] = o[u];
-  };
+    for (int i = 0; i < 16; ++i)
+      qf[2 * n + i / 8][i % 8] = 32 * n + 16 * (i / 8) < d ? (_Float16)(v[i] * f) : (_Float16)0.0f;
+  }
 
   if (cb < ce) {
-    key_pages(cb);
-    value_page(cb);
-    load_keys(cb);
-    load_values(cb);
-    store_keys(cb);
+    store_keys(cb, kc0);
+    store_keys(cb + 1, kc);
     clear_values(cb);
     store_values(cb);
     store_scales(cb);
-    key_pages(cb + 1);
-    load_keys(cb + 1);
-    store_keys(cb + 1);
-    key_pages(cb + 2);
-    value_page(cb + 1);
-    load_keys(cb + 2);
+    load_keys(cb + 2, kpg, kc);
     load_values(cb + 1);
-    key_pages(cb + 3);
+    key_pages(cb + 3, kpg);
     value_page(cb + 2);
   }
+  f32x16v s[2];
+  auto scores = [&](int c, int tt) {  // of 32 positions
+    f32x16v o;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 2 * ND; ++k) {
+      const f16x8 a = *reinterpret_cast<const f16x8 *>(&kt[c & 1][(32 * tt + krow) * KLD + 16 * k + 8 * g]);
+      o = mfma32(a, qf[k], o);
+    }
+    s[tt] = o;
+  };
   __syncthreads();
   if (wb == cb && cb < we) {
     scores(cb, 0);
@@ -919,9 +925,9 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
       const int j0 = c * kChunk;
       float ks[NR], lv[NR], inv[NR];
       bool there = true;
-      f16x8 ring[4];
+      f16x8 ring[RD];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) ring[k] = key_at(c + 1, k);
+      for (int k = 0; k < RD; ++k) ring[k] = key_at(c + 1, k);
 #pragma unroll
       for (int y = 0; y < NR; ++y) {
         const float4 z = sc[c & 1][y];
@@ -930,98 +936,82 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
         inv[y] = z.z;
         there = there && z.w != 0.0f;
       }
-      float ck[RC][NR], base[RC][NR], sum[RC][4];
+      float ck[NR], base[NR], sum[4];
+      if (!__all(there && j0 >= lo && j0 + kChunk <= hi)) {
+        int jg = j0 + 8 * g;
+        asm volatile("" : "+v"(jg));  // a branch: few tiles need it, so nothing of it is kept in registers
 #pragma unroll
-      for (int u = 0; u < RC; ++u) {
-        if (!__all(there && j0 >= lo[u] && j0 + kChunk <= hi[u])) {
-          int jg = j0 + 8 * g;
-          asm volatile("" : "+v"(jg));  // a branch: few tiles need it, so nothing of it is kept in registers
+        for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-          for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int j = jg + 32 * tt + 16 * (i >> 3) + (i & 7);
-              if (j < lo[u] || j >= hi[u] || sc[c & 1][ONE ? 0 : 2 * tt + (i >> 3)].w == 0.0f) s[tt][u][i] = -INFINITY;
-            }
-        }
-        float Mt = -INFINITY;
-#pragma unroll
-        for (int y = 0; y < NR; ++y) {
-          constexpr int E = 32 / NR;
-          float top = -INFINITY;
-#pragma unroll
-          for (int i = E * y; i < E * (y + 1); ++i) top = fmaxf(top, s[i >> 4][u][i & 15]);
-          // a factor of 0 (a row of tiny queries) would make NaN of -inf
-          ck[u][y] = fmaxf(cs[u] * ks[y], 0x1p-126f);
-          Mt = fmaxf(Mt, fmaf(top, ck[u][y], lv[y]));
-        }
-        Mt = max_halves(Mt);
-        if (__any(Mt > M[u] + kSlack)) {
-          const float Mn = fmaxf(M[u], Mt);
-          const float al = Mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(M[u] - Mn);
-          l[u] *= al;
-#pragma unroll
-          for (int n = 0; n < ND; ++n) acc[u][n] *= al;
-          M[u] = Mn;
-        }
-        const float up = kUp32 - (M[u] == -INFINITY ? 0.0f : M[u]);
-#pragma unroll
-        for (int y = 0; y < NR; ++y) base[u][y] = lv[y] + up;
+          for (int i = 0; i < 16; ++i) {
+            const int j = jg + 32 * tt + 16 * (i >> 3) + (i & 7);
+            if (j < lo || j >= hi || sc[c & 1][ONE ? 0 : 2 * tt + (i >> 3)].w == 0.0f) s[tt][i] = -INFINITY;
+          }
       }
-      // Steps of one product (per 32 rows) each, in this order: the operand of four steps ahead is read, the product is
+      float Mt = -INFINITY;
+#pragma unroll
+      for (int y = 0; y < NR; ++y) {
+        constexpr int E = 32 / NR;
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = E * y; i < E * (y + 1); ++i) top = fmaxf(top, s[i >> 4][i & 15]);
+        // a factor of 0 (a row of tiny queries) would make NaN of -inf
+        ck[y] = fmaxf(cs * ks[y], 0x1p-126f);
+        Mt = fmaxf(Mt, fmaf(top, ck[y], lv[y]));
+      }
+      Mt = max_halves(Mt);
+      if (__any(Mt > M + kSlack)) {
+        const float Mn = fmaxf(M, Mt);
+        const float al = Mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(M - Mn);
+        l *= al;
+#pragma unroll
+        for (int n = 0; n < ND; ++n) acc[n] *= al;
+        M = Mn;
+      }
+      const float up = kUp32 - (M == -INFINITY ? 0.0f : M);
+#pragma unroll
+      for (int y = 0; y < NR; ++y) base[y] = lv[y] + up;
+      // Steps of one product each, in this order: the operand of some steps ahead is read, the product is
       // issued, and what the vector unit does meanwhile follows.  First the scores of the next tile and this tile's
       // exponentials, 16 registers of scores at a time (the next tile's replace them), then the second products
       // and the widening of later tiles.
-      f16x8 w[RC][4];
-      f32x16v o[RC];
+      f16x8 w[4];
+      f32x16v o;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const int tt = k / (2 * ND), kk = k % (2 * ND);
         __builtin_amdgcn_sched_barrier(0);
-        const f16x8 a = ring[k % 4];
-        ring[k % 4] = k + 4 < KS ? key_at(c + 1, k + 4) : value_at(c, k + 4 - KS);
+        const f16x8 a = ring[k % RD];
+        ring[k % RD] = k + RD < KS ? key_at(c + 1, k + RD) : value_at(c, k + RD - KS);
         if (kk == 0) {
 #pragma unroll
-          for (int u = 0; u < RC; ++u)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[u][i] = 0.0f;
+          for (int i = 0; i < 16; ++i) o[i] = 0.0f;
         }
-#pragma unroll
-        for (int u = 0; u < RC; ++u) o[u] = mfma32(a, qf[u][kk], o[u]);
+        o = mfma32(a, qf[kk], o);
         // elements [e0, e1) of 16
         const int e0 = kk * 16 / (2 * ND), e1 = (kk + 1) * 16 / (2 * ND);
 #pragma unroll
-        for (int u = 0; u < RC; ++u) {
-#pragma unroll
-          for (int i = e0; i < e1; ++i) {
-            const int y = 2 * tt + (i >> 3);
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[tt][u][i], ck[u][y % NR], base[u][y % NR]));
-            sum[u][y] = (i & 7) ? sum[u][y] + e : e;
-            w[u][y][i & 7] = (_Float16)e;
-          }
+        for (int i = e0; i < e1; ++i) {
+          const int y = 2 * tt + (i >> 3);
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[tt][i], ck[y % NR], base[y % NR]));
+          sum[y] = (i & 7) ? sum[y] + e : e;
+          w[y][i & 7] = (_Float16)e;
         }
-        if (kk == 2 * ND - 1) {
-#pragma unroll
-          for (int u = 0; u < RC; ++u) s[tt][u] = o[u];
-        }
+        if (kk == 2 * ND - 1) s[tt] = o;
       }
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const int y = k / ND, n = k % ND;
         __builtin_amdgcn_sched_barrier(0);
-        const f16x8 a = ring[k % 4];
-        if (k + 4 < KS) ring[k % 4] = value_at(c, k + 4);
-#pragma unroll
-        for (int u = 0; u < RC; ++u) acc[u][n] = mfma32(a, w[u][y], acc[u][n]);
-        if (n == 0) {
-#pragma unroll
-          for (int u = 0; u < RC; ++u) l[u] = fmaf(sum[u][y], inv[y % NR], l[u]);
-        }
+        const f16x8 a = ring[(k + KS) % RD];
+        if (k + RD < KS) ring[(k + KS) % RD] = value_at(c, k + RD);
+        acc[n] = mfma32(a, w[y], acc[n]);
+        if (n == 0) l = fmaf(sum[y], inv[y % NR], l);
         // the widening, a piece at a time
         const int p0 = k * (KP + VP) / KS, p1 = (k + 1) * (KP + VP) / KS;
 #pragma unroll
         for (int i = p0; i < p1; ++i) {
-          if (i < KP) store_key(c + 2, i);
+          if (i < KP) store_key(c + 2, i, kc);
           else store_value(c + 1, i - KP);
         }
       }
@@ -1031,52 +1021,48 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
         scores(c + 1, 0);
         scores(c + 1, 1);
       }
-      store_keys(c + 2);
+      store_keys(c + 2, kc);
       store_values(c + 1);
     }
     // keys of tile c + 2 and values of tile c + 1 are in LDS, the loads of the tiles after them begin
     store_scales(c + 1);
-    load_keys(c + 3);
+    load_keys(c + 3, kpg, kc);
     load_values(c + 2);
-    key_pages(c + 4);
+    key_pages(c + 4, kpg);
     value_page(c + 3);
     __syncthreads();
   }
 
-#pragma unroll
-  for (int u = 0; u < RC; ++u) {
-    l[u] += __shfl_xor(l[u], 32);
-    const int r = rw + 32 * u + m;
-    if (splits > 1) {
-      if (r >= rows) continue;
-      if (l[u] != l[u]) M[u] = INFINITY;  // the maximum does not see NaN
-      float *o = P.part + ((((bh * P.rtiles + rt) * P.splits + split) * kWaves + wave) * RC + u) * part32_floats(ND);
-#pragma unroll
-      for (int n = 0; n < ND; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4 *>(o + ((n * 4 + i) * 64 + lane) * 4) =
-              f32x4{acc[u][n][4 * i], acc[u][n][4 * i + 1], acc[u][n][4 * i + 2], acc[u][n][4 * i + 3]};
-      if (g == 0) {
-        o[ND * 1024 + m] = M[u];
-        o[ND * 1024 + 32 + m] = l[u];
-      }
-      continue;
-    }
-    if (r >= rows) continue;
-    const RowAt at = row_at(A, C, q, h, r);
-    const float inv = l[u] == 0.0f ? 0.0f : 1.0f / l[u];
+  l += __shfl_xor(l, 32);
+  const int r = rw + m;
+  if (r >= rows) return;
+  if (splits > 1) {
+    if (l != l) M = INFINITY;  // the maximum does not see NaN
+    float *o = P.part + (((bh * P.rtiles + rt) * P.splits + split) * kWaves + wave) * part32_floats(ND);
 #pragma unroll
     for (int n = 0; n < ND; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = 32 * n + 8 * i + 4 * g;
-        const float z[4] = {acc[u][n][4 * i] * inv, acc[u][n][4 * i + 1] * inv, acc[u][n][4 * i + 2] * inv,
-                            acc[u][n][4 * i + 3] * inv};
-        if (c < d) store_o4(A, at.o + c, z);
-      }
-    if (A.lse && g == 0) A.lse[at.lse] = log_sum(M[u], l[u], kUp32);
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4 *>(o + ((n * 4 + i) * 64 + lane) * 4) =
+            f32x4{acc[n][4 * i], acc[n][4 * i + 1], acc[n][4 * i + 2], acc[n][4 * i + 3]};
+    if (g == 0) {
+      o[ND * 1024 + m] = M;
+      o[ND * 1024 + 32 + m] = l;
+    }
+    return;
   }
+  const RowAt at = row_at(A, C, q, h, r);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int n = 0; n < ND; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = 32 * n + 8 * i + 4 * g;
+      const float z[4] = {acc[n][4 * i] * inv, acc[n][4 * i + 1] * inv, acc[n][4 * i + 2] * inv,
+                          acc[n][4 * i + 3] * inv};
+      if (c < d) store_o4(A, at.o + c, z);
+    }
+  if (A.lse && g == 0) A.lse[at.lse] = log_sum(M, l, kUp32);
 }
 
 struct Plan {
@@ -1096,9 +1082,6 @@ int dim_tiles32(int d) {
   return t <= 2 ? 2 : t <= 3 ? 3 : t <= 4 ? 4 : t <= 6 ? 6 : 8;
 }
 
-// 64 rows of a wave share the operands read from LDS, as far as a wave's 512 registers hold their accumulators
-constexpr int row_tiles(int nd) { return 1; }
-
 Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   Plan p{};
   const int64_t rows = (int64_t)S.max_rows * A.group;
@@ -1107,7 +1090,7 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   const int64_t chunks = std::max<int64_t>(1, cdiv(len, kChunk));
   p.prompt = rows > 32 && A.type != KM_T_F32;
   p.nt = p.prompt ? dim_tiles32(C.d) : dim_tiles(C.d);
-  p.rt = p.prompt ? kWaves * row_tiles(p.nt) : rows > 16 && A.type != KM_T_F32 && p.nt <= 8 ? 2 : 1;
+  p.rt = p.prompt ? kWaves : rows > 16 && A.type != KM_T_F32 && p.nt <= 8 ? 2 : 1;
   p.rtiles = (int)cdiv(rows, (p.prompt ? 32 : 16) * p.rt);
   p.tiles = (int64_t)S.n * C.heads * p.rtiles;
   if (p.prompt) {
@@ -1160,8 +1143,8 @@ km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A,
   const dim3 grid((unsigned)(p.deal ? p.splits : p.tiles * p.splits));
   if (p.prompt) {
 #define KV_K(F, N)                                                                         \
-  C.page >= kChunk ? kv_prompt_kernel<F, N, row_tiles(N), true><<<grid, 64 * kWaves, 0, s>>>(P) \
-                   : kv_prompt_kernel<F, N, row_tiles(N), false><<<grid, 64 * kWaves, 0, s>>>(P)
+  C.page >= kChunk ? kv_prompt_kernel<F, N, true><<<grid, 64 * kWaves, 0, s>>>(P) \
+                   : kv_prompt_kernel<F, N, false><<<grid, 64 * kWaves, 0, s>>>(P)
 #define KV_N(N)                                                                                                 \
   case N:                                                                                                       \
     if (C.fmt == KM_KV_I8) KV_K(KM_KV_I8, N);                                                                   \
@@ -1186,8 +1169,8 @@ km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A,
   C.page >= kChunk ? kv_attend_kernel<F, N, R, Z, true><<<grid, 64 * kAttendWaves, 0, s>>>(P) \
                    : kv_attend_kernel<F, N, R, Z, false><<<grid, 64 * kAttendWaves, 0, s>>>(P)
 #define KV_R(F, N)                          \
-  if (A.type == KM_T_F32) KV_K(F, N, 1, 2); \
-  else if (p.rt == 2) KV_K(F, N, (N <= 8 ? 2 : 1), 1); \
+  if (A.type == KM_T_F32) KV_K(F, N, 1, 2);                       \
+  else if (N <= 8 && p.rt == 2) KV_K(F, N, (N <= 8 ? 2 : 1), 1); \
   else KV_K(F, N, 1, 1);
 #define KV_N(N)                                                                                         \
   case N:                                                                                               \

@@ -457,3 +457,95 @@ def test_offsets_past_32_bits():
         res.append([*km.kv_read(c, seqs), km.kv_attend(c, seqs, q)[0], km.kv_attend(c, one, q[:1].contiguous())[0]])
     for a, b in zip(*res):
         assert torch.equal(a, b)
+
+
+# Calls that are split up over workgroups: name, page, heads, group, d, lens, rows, window, extra table width (the width
+# stands for the length where max_len is not given, and with it for how a call is split).
+def _ragged(n, hi, seed):
+    return [int(x) for x in np.random.default_rng(seed).integers(0, hi, n)]
+
+
+SPLITS = {
+    "one_long": (64, 2, 2, 64, [5000], [1], 0, 0),
+    "one_long_rows": (32, 1, 8, 128, [3001], [4], 0, 0),
+    "one_window": (16, 2, 2, 80, [4000], [2], 1500, 0),
+    "few_even": (64, 2, 4, 64, [1500, 1100, 7], [1, 1, 1], 0, 0),
+    "dealt": (64, 2, 2, 64, _ragged(30, 900, 1), [1] * 30, 0, 150),
+    "dealt_70": (64, 2, 2, 64, _ragged(70, 400, 2), [1, 2, 0, 3, 1] * 14, 0, 80),
+    "dealt_130_window": (16, 1, 4, 64, _ragged(130, 200, 3), [1] * 130, 100, 300),
+    "dealt_two_tiles": (32, 2, 8, 128, _ragged(20, 500, 4), [4, 3] * 10, 0, 600),
+    "dealt_wide_heads": (64, 2, 2, 256, _ragged(25, 600, 5), [1] * 25, 0, 100),
+    "dealt_two_row_tiles": (64, 2, 6, 192, _ragged(15, 600, 6), [4] * 15, 0, 120),
+    "prompt_split": (64, 1, 2, 128, [1700, 900], [40, 33], 0, 0),
+    "prompt_split_small_pages": (16, 1, 4, 64, [1300], [50], 0, 0),
+    "prompt_split_window": (32, 2, 2, 80, [1500, 40], [64, 40], 700, 0),
+    "prompt_split_wide": (64, 1, 2, 256, [1100], [70], 0, 0),
+    "prompt_split_192": (128, 1, 4, 192, [1000], [30], 0, 0),
+}
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("name", list(SPLITS))
+def test_attend_split(name, fmt):
+    page, heads, group, d, lens, rows, window, wide = SPLITS[name]
+    say(f"kv_attend split {name} {fmt}")
+    s = Setup(fmt, page, heads, d, lens, rows, seed=300 + list(SPLITS).index(name), wide=wide)
+    q = s.normal((s.rows, heads * group, d), "bf16", 0.4)
+    _attend_check(s, q, "bf16", window=window, label=name)
+    if not window:
+        _attend_check(s, q, "bf16", causal=False, label=name + " whole")
+
+
+@pytest.mark.parametrize("name", ["one_long", "dealt_70"])
+def test_attend_split_f32(name):
+    page, heads, group, d, lens, rows, window, wide = SPLITS[name]
+    s = Setup("int8", page, heads, d, lens, rows, seed=400, wide=wide)
+    _attend_check(s, s.normal((s.rows, heads * group, d), "f32", 0.4), "f32", label=name)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_max_len_chooses_no_results(rows):
+    """A max_len that is too small, right or far too large: within the bound each time."""
+    km = _km()
+    s = Setup("int8", 16, 2, 64, [2500, 100, 900], [rows] * 3, seed=31)
+    q = s.normal((s.rows, 4, 64), "bf16")
+    for m in (1, 900, 2500, 0):
+        s.seqs = km.KvSeqs(s.seqs.table, s.seqs.lens, s.seqs.starts, rows=s.rows, max_rows=rows, max_len=m)
+        _attend_check(s, q, "bf16", label=f"max_len {m}")
+
+
+def test_workspace_from_the_pool():
+    """The C entry point without a workspace takes it from the pool: the same bits."""
+    torch = torch_cuda()
+    km = _km()
+    import ctypes as ct
+    from paper_2608_14648_amd import _kmq
+    s = Setup("fp8", 64, 2, 64, [4000], [1], seed=37)
+    q = s.normal((1, 4, 64), "f16")
+    want, _ = km.kv_attend(s.cache, s.seqs, q)
+    out = torch.empty_like(q)
+    qr, orow = (_kmq.KmKvRows(t.data_ptr(), t.stride(0), t.stride(1)) for t in (q, out))
+    assert _kmq.lib().kv_attend_bytes(s.cache._ref, s.seqs._ref, 4, 1, 0, 2) > 0
+    st = _kmq.lib().kv_attend(s.cache._ref, s.seqs._ref, ct.addressof(qr), 4, 0.125, 1, 0, ct.addressof(orow), 2, None,
+                              None, 0, torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_example(fmt):
+    """The example's three calls together.  A value of a page is within 1/254 of its largest one (int8), 1/16 of itself
+    (fp8, about 1/40 on average); keys of a normal distribution then come back within 2 % and 4 %, and what
+    attention averages of them within 5 %."""
+    torch = torch_cuda()
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "kv_cache.py")
+    spec = importlib.util.spec_from_file_location("kv_cache_example", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    r = ex.main(steps=6, dtype=torch.int8 if fmt == "int8" else torch.float8_e4m3fn, say=say)
+    assert r["read"] <= (0.02 if fmt == "int8" else 0.04)
+    assert r["prompt"] <= 0.05 and r["token"] <= 0.05
+    assert all(b <= a for a, b in r["cost"])
