@@ -74,13 +74,18 @@ struct PageJob {
   int lead;     // rows from row0 on that fall before position 0: zeros when read (the first page's workgroups write them)
 };
 
-// Job of workgroup x: touched page t of head h of sequence b.
-__device__ __forceinline__ bool page_job(const KvCache &C, const KvSeqs &S, int64_t x, int touched, int *h,
+// Job of workgroup x: keys or values of touched page t of head h of sequence b.  A page's heads lie eight workgroups apart, on
+// one XCD: their rows lie side by side (64 thousand tokens, 8 heads of 128, written and read back: 197 us, spread 205).
+__device__ __forceinline__ bool page_job(const KvCache &C, const KvSeqs &S, uint32_t x, int touched, bool *values, int *h,
                                          PageJob *j) {
-  *h = (int)(x % C.heads);
-  x /= C.heads;
-  const int t = (int)(x % touched);
-  const int b = (int)(x / touched);
+  uint32_t y = x >> 3;
+  const uint32_t part = y % (2u * C.heads);
+  y = (y / (2u * C.heads)) * 8 + (x & 7);
+  *values = part & 1;
+  *h = (int)(part >> 1);
+  const int t = (int)(y % (uint32_t)touched);
+  const int b = (int)(y / (uint32_t)touched);
+  if (b >= S.n) return false;
   KvSeq q;
   if (!kv_seq(S, C.page, b, &q)) return false;
   const int first = max(q.len - q.n, 0);  // rows before position 0 have no place
@@ -168,6 +173,19 @@ __device__ __forceinline__ void advance(Place &p, int per, int dr, int dc) {
   }
 }
 
+// Item i of a page's values: 16 tokens g of the four dims from c on.  Up to four groups of tokens (64 bytes of a dim's row)
+// lie side by side, then the dims (rows of up to 128 bytes and more), then the other four groups of a page of 128.
+__device__ __forceinline__ void group_of(int i, int ng, int quads, int *g, int *c) {
+  const int bits = ng >= 4 ? 2 : ng - 1;  // of 1, 2 or 4 groups
+  int q = i >> bits;
+  *g = i & ((1 << bits) - 1);
+  if (q >= quads) {
+    q -= quads;
+    *g += 4;
+  }
+  *c = 4 * q;
+}
+
 // The bytes y of four dwords as one dword each: a 4 x 4 transpose.
 __device__ __forceinline__ void turn4(const uint32_t *a, uint32_t *o) {
   const uint32_t x = __builtin_amdgcn_perm(a[1], a[0], 0x05010400u), y = __builtin_amdgcn_perm(a[3], a[2], 0x05010400u);
@@ -185,10 +203,10 @@ template <int FMT, int TYPE>
 __global__ __launch_bounds__(1024) void kv_write_kernel(KvCache C, KvSeqs S, KvRows kr, KvRows vr, int touched) {
   extern __shared__ uint32_t turn[];  // values: codes of the new rows, [token][turn_ld]
   __shared__ uint32_t sh[16];
-  const bool values = blockIdx.x & 1;
+  bool values;
   int h;
   PageJob j;
-  if (!page_job(C, S, blockIdx.x >> 1, touched, &h, &j) || j.i1 == 0 || j.pg < 0) return;
+  if (!page_job(C, S, blockIdx.x, touched, &values, &h, &j) || j.i1 == 0 || j.pg < 0) return;
   const KvRows &src = values ? vr : kr;
   const int d = C.d, t = threadIdx.x, T = blockDim.x;
   const int per = d / 8, rows = j.i1 - j.i0;  // items of 8 dims in a row
@@ -292,9 +310,10 @@ __global__ __launch_bounds__(1024) void kv_write_kernel(KvCache C, KvSeqs S, KvR
   }
   // 16 tokens of four dims at a time, neighbouring threads the tokens of a dim's row.  What lies in a group before i0 is
   // coded again or stays, what lies behind i1 stays.
-  const int ng = C.page / 16, gs = C.shift - 4;
+  const int ng = C.page / 16;
   for (int i = t; i < ng * (d / 4); i += T) {
-    const int g = i & (ng - 1), c = (i >> gs) * 4;
+    int g, c;
+    group_of(i, ng, d / 4, &g, &c);
     const int k0 = g * 16 - j.i0;  // row of its first token
     if (g * 16 >= j.i1 || (!again && g * 16 + 16 <= j.i0)) continue;
     uint8_t *o = dst + c * C.page + g * 16;
@@ -341,10 +360,10 @@ __device__ __forceinline__ float value(float code, float s) {
 
 template <int FMT, int TYPE>
 __global__ __launch_bounds__(1024) void kv_read_kernel(KvCache C, KvSeqs S, KvRows kr, KvRows vr, int touched) {
-  const bool values = blockIdx.x & 1;
+  bool values;
   int h;
   PageJob j;
-  if (!page_job(C, S, blockIdx.x >> 1, touched, &h, &j)) return;
+  if (!page_job(C, S, blockIdx.x, touched, &values, &h, &j)) return;
   const KvRows &out = values ? vr : kr;
   const int d = C.d, t = threadIdx.x, T = blockDim.x;
   for (int i = t; i < j.lead * (d / 4); i += T) {
@@ -388,9 +407,10 @@ __global__ __launch_bounds__(1024) void kv_read_kernel(KvCache C, KvSeqs S, KvRo
     return;
   }
   // 16 tokens of four dims: four loads, sixteen rows of four values; neighbouring threads the tokens of a dim's row
-  const int ng = C.page / 16, gs = C.shift - 4;
+  const int ng = C.page / 16;
   for (int i = t; i < ng * (d / 4); i += T) {
-    const int g = i & (ng - 1), c = (i >> gs) * 4;
+    int g, c;
+    group_of(i, ng, d / 4, &g, &c);
     if (g * 16 >= j.i1 || g * 16 + 16 <= j.i0) continue;
     u32x4 w[4];
 #pragma unroll
@@ -428,7 +448,9 @@ int move_threads(const KvCache &C, const KvSeqs &S) {
 
 }  // namespace
 
-int64_t kv_move_blocks(const KvCache &C, const KvSeqs &S) { return 2 * (int64_t)S.n * touched_pages(C, S) * C.heads; }
+int64_t kv_move_blocks(const KvCache &C, const KvSeqs &S) {
+  return cdiv((int64_t)S.n * touched_pages(C, S), 8) * 8 * 2 * C.heads;
+}
 
 km_status launch_kv_write(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v, int type, hipStream_t s) {
   const int touched = touched_pages(C, S);
