@@ -6,8 +6,8 @@
 // are different workgroups.  Values lie with their dims first (the attention's second product contracts tokens), so
 // their codes turn through LDS on the way in and in registers on the way out.
 //
-// Both are bound by HBM: 3 bytes per 16-bit element, 4.6 and 4.7 TB/s for 74631 tokens of 8 heads of 128 (100 and 96 us;
-// a large copy 4.7).  One token: 3.4 and 3.7 us.  The rows of a page are read once and kept in registers (a
+// Both are bound by HBM: 3 bytes per 16-bit element, 4.6 and 5.7 TB/s for 74631 tokens of 8 heads of 128 (100 and 80 us;
+// a large copy 4.7).  One token: 3.1 and 3.7 us.  The rows of a page are read once and kept in registers (a
 // workgroup has as many threads as that takes), its largest magnitude is taken on the bit patterns, and only a page that
 // holds infinities or NaN looks at them one by one.
 #include "kv.hpp"
@@ -76,7 +76,8 @@ struct PageJob {
 };
 
 // Job of workgroup x: keys or values of touched page t of head h of sequence b.  A page's heads lie eight workgroups apart, on
-// one XCD: their rows lie side by side (64 thousand tokens, 8 heads of 128, written and read back: 197 us, spread 205).
+// one XCD: their rows lie side by side (74631 tokens of 8 heads of 128, written and read back: 197 us, spread 205, both
+// before rows were read whole).
 __device__ __forceinline__ bool page_job(const KvCache &C, const KvSeqs &S, uint32_t x, int touched, bool *values, int *h,
                                          PageJob *j) {
   uint32_t y = x >> 3;
