@@ -1124,15 +1124,18 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
     p.per = (int)std::max<int64_t>(8, cdiv(p.tiles * chunks, 512));
     p.spread = p.tiles * p.rt < 256;
   } else {
-    // Short contexts, or rows enough that tiles fill the card several times: a workgroup for each tile and no join.  A
+    // Short contexts, or tiles enough to fill the card several times: a workgroup for each tile and no join.  A
     // workgroup takes 6.5 us and 1.7 more per 256 positions (8 heads of 128); splitting it up and joining takes 14 us up to
     // some 4096 positions.  Where that leaves every workgroup little to do, even splits; where it streams for long, what
-    // differing lengths leave idle counts for more, and tiles are dealt out (64 sequences of 1 to 16384 tokens: 194 us, even
-    // splits 225; 16 sequences behind a window of 4096: 39 us, even splits 28).  As many workgroups as run at a time.
+    // differing lengths leave idle counts for more, and tiles are dealt out.  8 heads of 128, lengths from 1 on:
+    //   64 sequences up to 16384 (512 tiles): 194 us dealt out, 225 even splits; up to 4000: 56, a workgroup each 61
+    //   256 up to 4000 (2048 tiles): 242 us dealt out, 213 a workgroup each; 128 up to 4000: 130 either way
+    //   16 behind a window of 4096, 4 heads (64 tiles): 39 us dealt out, 28 even splits
+    // As many workgroups as run at a time.
     const int64_t cap = (int64_t)S.max_pages * C.page / kChunk + 1 + kTileCost;  // whatever max_len says
     const int64_t most = p.nt <= 8 ? 512 : 256;
     p.spread = p.tiles * p.rt < 256;
-    if (p.rtiles > 4 || chunks <= (p.tiles < 256 ? 16 : 32)) {
+    if (p.rtiles > 4 || p.tiles >= 2 * most || chunks <= (p.tiles < 256 ? 16 : 32)) {
       p.per = (int)chunks;
     } else if (p.tiles * chunks <= 16 * most || S.n == 1 || p.tiles * cap >= INT32_MAX) {
       p.per = (int)std::max<int64_t>(kAttendWaves, cdiv(p.tiles * chunks, most));

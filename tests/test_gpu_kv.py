@@ -472,7 +472,8 @@ SPLITS = {
     "few_even": (64, 2, 4, 64, [1500, 1100, 7], [1, 1, 1], 0, 0),
     "dealt": (64, 2, 2, 64, _ragged(30, 900, 1), [1] * 30, 0, 150),
     "dealt_70": (64, 2, 2, 64, _ragged(70, 400, 2), [1, 2, 0, 3, 1] * 14, 0, 80),
-    "dealt_130_window": (16, 1, 4, 64, _ragged(130, 200, 3), [1] * 130, 100, 300),
+    "dealt_130_window": (16, 1, 4, 64, _ragged(100, 200, 3) + [4300] + _ragged(29, 200, 7), [1] * 130, 4000, 300),
+    "many_tiles": (16, 8, 1, 64, _ragged(140, 60, 8), [1] * 140, 0, 100),
     "dealt_two_tiles": (32, 2, 8, 128, _ragged(20, 500, 4), [4, 3] * 10, 0, 600),
     "dealt_wide_heads": (64, 2, 2, 256, _ragged(25, 600, 5), [1] * 25, 0, 100),
     "dealt_two_row_tiles": (64, 2, 6, 192, _ragged(15, 600, 6), [4] * 15, 0, 120),
