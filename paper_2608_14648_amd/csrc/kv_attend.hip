@@ -217,7 +217,7 @@ __device__ __forceinline__ int deal_run(const AttendArgs &P, int all) {
   return max((int)(((uint32_t)all + P.splits - 1) / (uint32_t)P.splits), P.per);
 }
 
-constexpr int kAttendWaves = 4;
+constexpr int kAttendWaves = 4, kWideWaves = 8;  // of a workgroup (see plan)
 
 // LDS of a workgroup: maxima and sums of each wave's rows, then each wave's accumulators.
 template <int RT, int NT>
@@ -227,11 +227,10 @@ struct AttendWave {
 };
 
 // Chunks [cb, ce) of rows [r0, ...) of a sequence's head; the results, or where part is given the sums for the join.
-template <int FMT, int NT, int RT, int NS, bool ONE>
+template <int FMT, int NT, int RT, int NS, bool ONE, int W>
 __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q, int b, int h, int r0, int cb, int ce,
                                             float *part, AttendWave<RT, NT> *sh) {
   constexpr int NP = (NT + 3) / 4;  // groups of 64 dims
-  constexpr int W = kAttendWaves;
   const KvCache &C = P.C;
   const KvAttend &A = P.A;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
@@ -493,9 +492,9 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
   }
 }
 
-template <int FMT, int NT, int RT, int NS, bool ONE>
-__global__ __launch_bounds__(64 * kAttendWaves, NT <= 8 ? 2 : 1) void kv_attend_kernel(AttendArgs P) {
-  __shared__ AttendWave<RT, NT> sh[kAttendWaves];
+template <int FMT, int NT, int RT, int NS, bool ONE, int W>
+__global__ __launch_bounds__(64 * W, NT <= 8 ? 2 : 1) void kv_attend_kernel(AttendArgs P) {
+  __shared__ AttendWave<RT, NT> sh[W];
   constexpr int TR = 16 * RT;
   KvSeq q;
   if (!P.deal) {  // a workgroup per tile and split
@@ -510,7 +509,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, NT <= 8 ? 2 : 1) void kv_attend_
     const int r0 = rt * TR, rows = q.n * P.A.group;
     int cb, ce, of;
     if (r0 < rows && tile_span(P, q, r0, min(r0 + TR, rows), split, &cb, &ce, &of))
-      attend_tile<FMT, NT, RT, NS, ONE>(P, q, b, h, r0, cb, ce, of > 1 ? part : nullptr, sh);
+      attend_tile<FMT, NT, RT, NS, ONE, W>(P, q, b, h, r0, cb, ce, of > 1 ? part : nullptr, sh);
     return;
   }
   const DealScan o = deal_all(P, TR);
@@ -531,7 +530,7 @@ __global__ __launch_bounds__(64 * kAttendWaves, NT <= 8 ? 2 : 1) void kv_attend_
         // a tile that began in another workgroup, or one that is not finished here
         float *part = c1 - c0 == s.n ? nullptr
                                      : P.part + ((int64_t)blockIdx.x * 2 + (c0 == 0)) * RT * part_floats(NT);
-        attend_tile<FMT, NT, RT, NS, ONE>(P, q, b, tile / rtiles, tile % rtiles * TR, s.c0 + c0, s.c0 + c1, part, sh);
+        attend_tile<FMT, NT, RT, NS, ONE, W>(P, q, b, tile / rtiles, tile % rtiles * TR, s.c0 + c0, s.c0 + c1, part, sh);
       }
       left -= take;
       skip = 0;
@@ -1095,6 +1094,7 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
 struct Plan {
   bool prompt;
   int nt, rt, rtiles, deal, splits, per;
+  bool wide;  // kWideWaves waves to a workgroup of kv_attend_kernel
   int spread;  // the join has a workgroup per accumulator of a lane
   int64_t tiles;
 };
@@ -1126,23 +1126,42 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   } else {
     // Short contexts, or tiles enough to fill the card several times: a workgroup for each tile and no join.  A
     // workgroup takes 6.5 us and 1.7 more per 256 positions (8 heads of 128); splitting it up and joining takes 14 us up to
-    // some 4096 positions.  Where that leaves every workgroup little to do, even splits; where it streams for long, what
-    // differing lengths leave idle counts for more, and tiles are dealt out.  8 heads of 128, lengths from 1 on:
+    // some 4096 positions, more where tiles nearly fill the card by themselves: pieces of them are then short, and there are
+    // many to join.  Where a workgroup per tile leaves every workgroup little to do, even splits; where it streams for long,
+    // what differing lengths leave idle counts for more, and tiles are dealt out.  8 heads of 128, lengths from 1 on:
     //   64 sequences up to 16384 (512 tiles): 194 us dealt out, 225 even splits; up to 4000: 56, a workgroup each 61
     //   256 up to 4000 (2048 tiles): 242 us dealt out, 213 a workgroup each; 128 up to 4000: 130 either way
+    //   31 up to 3000 (248 tiles): 37 us dealt out, 27 a workgroup each; 31 of 6000 91 and 71; 24 up to 8000: 47 and 52
+    //   16 up to 1500 (128 tiles): 19 us even splits, 15 a workgroup each; up to 3000: 23 and 25
+    //   8 up to 1500 (64 tiles): 14 us even splits, 15 a workgroup each
     //   16 behind a window of 4096, 4 heads (64 tiles): 39 us dealt out, 28 even splits
+    // Workgroups of eight waves (accumulators of up to 128 dims, 16-bit types) have the loads of a CU in flight with half the
+    // tiles' beginnings, ends and pieces to join, but wait for each other at both:
+    //   a tile each, 32 up to 2000: 23.2 us with four waves, 20.8 with eight; one of 300 7.0 and 7.2 (64 dims)
+    //   even splits, one head, 100000 positions: 22.7 and 17.9; one sequence of 1500, 8 heads: 11.3 and 12.9
+    //   dealt out, 64 up to 16384: 194 and 187; 32 up to 8000: 48 and 51; 2 up to 29000 of 16 heads (32 tiles): 26 and 27;
+    //   32 rows to a tile, 64 up to 4000: 68 and 104
     // As many workgroups as run at a time.
     const int64_t cap = (int64_t)S.max_pages * C.page / kChunk + 1 + kTileCost;  // whatever max_len says
     const int64_t most = p.nt <= 8 ? 512 : 256;
+    const bool eight = p.nt <= 8 && A.type != KM_T_F32;
     p.spread = p.tiles * p.rt < 256;
-    if (p.rtiles > 4 || p.tiles >= 2 * most || chunks <= (p.tiles < 256 ? 16 : 32)) {
+    const int64_t alone = p.tiles > 256    ? 32  // the most chunks of a tile that is not split up
+                          : p.tiles >= 192 ? (eight ? 96 : 48)
+                          : p.tiles >= 128 ? (eight && p.rt == 1 ? 32 : 24)
+                                           : 16;
+    if (p.rtiles > 4 || p.tiles >= 2 * most || chunks <= alone) {
+      p.wide = eight && p.tiles <= 256 && chunks > 2 * kAttendWaves;
       p.per = (int)chunks;
     } else if (p.tiles * chunks <= 16 * most || S.n == 1 || p.tiles * cap >= INT32_MAX) {
-      p.per = (int)std::max<int64_t>(kAttendWaves, cdiv(p.tiles * chunks, most));
+      p.wide = eight && p.nt == 8 && (p.tiles * chunks > kAttendWaves * most || chunks > 1024);
+      p.per = (int)(p.wide ? std::max<int64_t>(kWideWaves, cdiv(2 * p.tiles * chunks, most))
+                           : std::max<int64_t>(kAttendWaves, cdiv(p.tiles * chunks, most)));
     } else {
       p.deal = 1;
-      p.per = 2 * kAttendWaves;
-      p.splits = (int)std::min<int64_t>(most, cdiv(p.tiles * chunks, p.per));
+      p.wide = eight && p.nt == 8 && p.rt == 1 && chunks >= 160 && p.tiles >= 128;
+      p.per = 2 * (p.wide ? kWideWaves : kAttendWaves);
+      p.splits = (int)std::min<int64_t>(p.wide ? most / 2 : most, cdiv(p.tiles * chunks, p.per));
       return p;
     }
   }
@@ -1197,13 +1216,20 @@ km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A,
     KMQ_LAUNCH_CHECK("kv_attend");
     return KM_OK;
   }
-#define KV_K(F, N, R, Z)                                                              \
-  C.page >= kChunk ? kv_attend_kernel<F, N, R, Z, true><<<grid, 64 * kAttendWaves, 0, s>>>(P) \
-                   : kv_attend_kernel<F, N, R, Z, false><<<grid, 64 * kAttendWaves, 0, s>>>(P)
-#define KV_R(F, N)                          \
-  if (A.type == KM_T_F32) KV_K(F, N, 1, 2);                       \
-  else if (N <= 8 && p.rt == 2) KV_K(F, N, (N <= 8 ? 2 : 1), 1); \
-  else KV_K(F, N, 1, 1);
+#define KV_K(F, N, R, Z, W)                                                              \
+  C.page >= kChunk ? kv_attend_kernel<F, N, R, Z, true, W><<<grid, 64 * (W), 0, s>>>(P) \
+                   : kv_attend_kernel<F, N, R, Z, false, W><<<grid, 64 * (W), 0, s>>>(P)
+#define KV_W(F, N, R)                                                       \
+  if (N <= 8 && p.wide) KV_K(F, N, R, 1, (N <= 8 ? kWideWaves : kAttendWaves)); \
+  else KV_K(F, N, R, 1, kAttendWaves);
+#define KV_R(F, N)                                                \
+  if (A.type == KM_T_F32) {                                       \
+    KV_K(F, N, 1, 2, kAttendWaves);                               \
+  } else if (N <= 8 && p.rt == 2) {                               \
+    KV_W(F, N, (N <= 8 ? 2 : 1))                                  \
+  } else {                                                        \
+    KV_W(F, N, 1)                                                 \
+  }
 #define KV_N(N)                                                                                         \
   case N:                                                                                               \
     if (C.fmt == KM_KV_I8) {                                                                            \
@@ -1227,6 +1253,7 @@ km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A,
   }
 #undef KV_N
 #undef KV_R
+#undef KV_W
 #undef KV_K
 #undef KV_J
   KMQ_LAUNCH_CHECK("kv_attend");
