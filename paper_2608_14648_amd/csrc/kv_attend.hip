@@ -19,8 +19,8 @@
 // product, whose other operand is 16 contiguous bytes of one dim of the value page.  A page is 16 tokens or more, so
 // a lane's 16 positions share one page and its scales.
 //
-// Measured (8 cache heads of 128, bf16): one sequence of 131071 tokens 45 us for 268 MB and 6 to join; 64 sequences of 1 to
-// 16384 tokens 183 us for 1028 MB, 5.6 TB/s, where a read alone reaches 6.3.  A chunk of a wave is about 520 vector
+// Measured (8 cache heads of 128, bf16): one sequence of 131071 tokens 45 us for 268 MB and 5 to join; 64 sequences of 1 to
+// 16384 tokens 179 us for 1028 MB, 5.7 TB/s, where a read alone reaches 6.3.  A chunk of a wave is about 520 vector
 // instructions, 320 of them the widening of int8 codes (five per four codes, e4m3 two), and 32 products.
 #include "kv.hpp"
 
