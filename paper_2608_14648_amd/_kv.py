@@ -112,7 +112,9 @@ def _rows_of(t: torch.Tensor, name: str, seqs: KvSeqs, heads: int, d: int, dtype
         row = 0
     if heads == 1:
         head = 0
-    if written and ((row < d and seqs.rows > 1) or (head < d and heads > 1)):
+    if written and ((row < d and seqs.rows > 1) or (head < d and heads > 1) or
+                    (seqs.rows > 1 and heads > 1 and  # the axis of the larger stride steps over the other one
+                     (row < (heads - 1) * head + d if row >= head else head < (seqs.rows - 1) * row + d))):
         raise ValueError(f"{name} is written: its rows and heads must not overlap")
     return KmKvRows(t.data_ptr(), row, head)
 

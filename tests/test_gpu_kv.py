@@ -459,6 +459,25 @@ def test_offsets_past_32_bits():
         assert torch.equal(a, b)
 
 
+def test_written_rows_must_not_overlap():
+    torch = torch_cuda()
+    km = _km()
+    s = Setup("int8", 16, 2, 64, [40], [40], seed=41)
+    flat = torch.zeros(40 * 64 * 3, dtype=torch.bfloat16, device="cuda")
+    for st in ((64, 64), (128, 0), (0, 64), (64, 128)):  # two heads of 64 dims each, 40 rows
+        bad = flat.as_strided((40, 2, 64), (*st, 1))
+        with pytest.raises(ValueError, match="overlap"):
+            km.kv_read(s.cache, s.seqs, k=bad)
+        with pytest.raises(ValueError, match="overlap"):
+            km.kv_attend(s.cache, s.seqs, torch.zeros(40, 2, 64, dtype=torch.bfloat16, device="cuda"), out=bad)
+    want = km.kv_read(s.cache, s.seqs)
+    heads_first = torch.zeros(2, 40, 64, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    apart = torch.zeros(40, 2, 72, dtype=torch.bfloat16, device="cuda")[:, :, :64]
+    for k in (heads_first, apart):
+        got = km.kv_read(s.cache, s.seqs, k=k, v=torch.empty_like(want[1]))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 # Calls that are split up over workgroups: name, page, heads, group, d, lens, rows, window, extra table width (the width
 # stands for the length where max_len is not given, and with it for how a call is split).
 def _ragged(n, hi, seed):
