@@ -427,7 +427,7 @@ typedef struct km_kv_cache {
 /*
  * The sequences of a call.  Rows of a call (keys and values, queries, results) are packed over the sequences; those of
  * sequence b are the LAST positions of it, up to position lens[b] - 1.
- *   table: int32[n][table_ld], pages of each sequence, table_ld >= max_pages >= 1,
+ *   table: int32[n][table_ld], pages of each sequence, table_ld >= max_pages >= 1 (or 0: one row for all sequences),
  *   max_pages * page <= 2^30.  lens: int32[n], tokens of each
  *   sequence, the call's own included.  starts: int32[n + 1], rows starts[b] .. starts[b + 1] - 1 are sequence b's;
  *   NULL: every sequence has max_rows rows and rows = n * max_rows.  rows: rows of all sequences.  max_rows: the most

@@ -59,7 +59,8 @@ def kv_cache(pages: int, heads: int, d: int, page: int = 64, dtype: torch.dtype 
 class KvSeqs:
     """The sequences of a call (mirrors ``km_kv_seqs``).
 
-    table: int32 [n, max_pages], the pages of each sequence; lens: int32 [n], tokens of each one, the call's own
+    table: int32 [n, max_pages], the pages of each sequence (one row expanded to n: all of them have the same pages, which
+    may be read and attended, not written); lens: int32 [n], tokens of each one, the call's own
     included; starts: int32 [n + 1], rows starts[b] .. starts[b + 1] of a call are the last positions of sequence b, or
     None: rows / n rows each.  rows: rows of all sequences (default n, one each); max_rows: the most of one sequence
     (default rows / n without starts, else rows); max_len: the longest of lens where the program knows it (it chooses
@@ -86,11 +87,14 @@ class KvSeqs:
                 max_rows = rows // n if n else 0
             if rows != n * max_rows:
                 raise ValueError("without starts rows must be n * max_rows")
+        ld = table.stride(0)
+        if n <= 1:  # the stride of an axis of one is of no meaning
+            ld = table.shape[1]
+        elif ld != 0 and ld < table.shape[1]:
+            raise ValueError(f"table's rows must not overlap in part (stride {ld}, {table.shape[1]} pages)")
         self.table, self.lens, self.starts = table, lens, starts
         self.n, self.rows, self.max_rows, self.max_len = n, rows, max_rows, max_len
         self.device = table.device
-        # a table of one row may have any stride
-        ld = max(table.stride(0), table.shape[1])
         self._c = KmKvSeqs(n, table.shape[1], table.data_ptr(), ld, lens.data_ptr(),
                            None if starts is None else starts.data_ptr(), rows, max_rows, max_len)
         self._ref = ct.addressof(self._c)

@@ -1177,7 +1177,8 @@ static km_status check_seqs(const km_kv_seqs *s, const KvCache &c, KvSeqs *o) {
   *o = KvSeqs{};
   if (s->n == 0 || s->rows == 0 || s->max_rows == 0) return KM_OK;
   KMQ_CHECK(s->table != nullptr && s->lens != nullptr, KM_EINVAL, "NULL argument");
-  KMQ_CHECK(s->max_pages >= 1 && s->table_ld >= s->max_pages, KM_EINVAL, "need table_ld >= max_pages >= 1");
+  KMQ_CHECK(s->max_pages >= 1 && (s->table_ld >= s->max_pages || s->table_ld == 0), KM_EINVAL,
+            "need table_ld >= max_pages >= 1 (or table_ld = 0)");
   KMQ_CHECK((int64_t)s->max_pages * c.page <= ((int64_t)1 << 30), KM_EINVAL, "max_pages * page = %lld above 2^30",
             (long long)s->max_pages * c.page);
   KMQ_CHECK(s->starts != nullptr || s->rows == (int64_t)s->n * s->max_rows, KM_EINVAL,

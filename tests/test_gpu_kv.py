@@ -592,3 +592,19 @@ def test_example(fmt):
     assert r["read"] <= (0.02 if fmt == "int8" else 0.04)
     assert r["prompt"] <= 0.05 and r["token"] <= 0.05
     assert all(b <= a for a, b in r["cost"])
+
+
+def test_one_table_row_for_all_sequences():
+    """A prefix that several sequences share, its row of the table expanded: read and attended as with a row for each."""
+    torch, km = torch_cuda(), _km()
+    s = Setup("int8", 16, 2, 64, [70], [70], seed=43)
+    lens = torch.tensor([70, 33, 1, 64], dtype=torch.int32, device="cuda")
+    one = torch.from_numpy(s.table).cuda()
+    for rows in (1, 40):
+        q = s.normal((4 * rows, 4, 64), "bf16")
+        res = []
+        for table in (one.expand(4, -1), one.repeat(4, 1)):
+            seqs = km.KvSeqs(table, lens, None, rows=4 * rows)
+            res.append([*km.kv_read(s.cache, seqs), *km.kv_attend(s.cache, seqs, q, lse=True)])
+        for a, b in zip(*res):
+            assert torch.equal(a, b)

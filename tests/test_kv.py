@@ -183,3 +183,24 @@ def test_binding_refuses_host_tensors():
         km.kv_cache(1, 1, 16, dtype=torch.float32, device="cpu")
     with pytest.raises(ValueError):
         km.KvSeqs(torch.zeros((1, 1), dtype=torch.int32), torch.zeros(1, dtype=torch.int32))
+
+
+@needs_lib
+def test_table_rows_of_one_address_or_apart(kmq):
+    """The stride of the descriptor is the table's own: 0 for one row expanded to all sequences; rows that overlap in part are
+    refused.  (Fake tensors: shapes and strides without memory.)"""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    import paper_2608_14648_amd as km
+    with FakeTensorMode():
+        def table(n, width, row):
+            return torch.empty(n * max(row, 1) + width, dtype=torch.int32, device="cuda:0").as_strided((n, width), (row, 1))
+        lens = torch.empty(3, dtype=torch.int32, device="cuda:0")
+        for row, ld in ((0, 0), (5, 5), (8, 8)):
+            assert km.KvSeqs(table(3, 5, row), lens)._c.table_ld == ld
+        for row in (1, 4):
+            with pytest.raises(ValueError, match="overlap"):
+                km.KvSeqs(table(3, 5, row), lens)
+        assert km.KvSeqs(table(1, 5, 0), lens[:1])._c.table_ld == 5
+    c, s, _ = (ct.byref(x) for x in _args(kmq, seqs=dict(table_ld=0)))
+    assert kmq.lib().kv_attend_bytes(c, s, 4, 1, 0, 1) == 0
