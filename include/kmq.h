@@ -489,8 +489,8 @@ km_status kv_read(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_
  *   A row that sees no position gets zeros and -infinity.
  *   q_heads: a multiple of heads; max_rows * q_heads / heads < 2^30.  scale: finite, > 0.
  *   ws (nullable): kv_attend_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the
- *   pool.  Codes of positions inside a sequence have to be finite and their pages' scales finite and > 0 (kv_write makes
- *   no others); what lies behind its end is not looked at.
+ *   pool.  Codes of positions inside a sequence have to be finite and their pages' scales finite and not below 2^-100
+ *   (kv_write makes no others); what lies behind its end is not looked at.
  *   fp32 queries: products and weights in two halves each (about 22 bits); 16-bit ones: their own bits, weights rounded to
  *   fp16; sums, maxima and normalisation in fp32.
  *   The result does not depend on scheduling.

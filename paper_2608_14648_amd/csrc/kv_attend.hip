@@ -6,7 +6,7 @@
 //
 //   t_ij = c_i ks_j <q'_i, kcode_j> + log2 vs_j   c_i = scale log2(e) 2^e_i, q'_i = q_i 2^-e_i in fp16
 //   w_ij = 2^(t_ij - M_i + 15)                    M_i = the running maximum of t_ij
-//   o_i  = (sum_j w_ij vcode_j) / l_i             l_i = sum_j w_ij / vs_j
+//   o_i  = (sum_j w_ij vcode_j) / l_i             l_i = sum_j w_ij / vs_j  (in units of 2^18, see kUnit)
 //
 // q'_i is the row times the power of two that brings its largest value to [2^13, 2^14): a 16-bit value stays exact down
 // to 2^-27 of the row's largest.  Taking the maximum of the weight with its value scale keeps w in fp16's range for
@@ -30,6 +30,9 @@ namespace {
 constexpr int kChunk = 64;    // positions per step of a wave
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kUp = 15.0f;  // weights are at most 2^15
+// l is kept in units of 2^18.  kv_write gives scales from 2^-100 (a page of zeros) to 2^121, so a position of the
+// largest weight, 2^8 to 2^15, adds 2^97 to 2^-131 to it: sums of 2^30 positions stay below 2^128.
+constexpr float kUnit = 0x1p-18f;
 
 struct AttendArgs {
   KvCache C;
@@ -102,9 +105,20 @@ __device__ __forceinline__ void q_scale(float top, float scale, float *f, float 
   *c = scale * kLog2e * __uint_as_float((uint32_t)(127 - up) << 23);
 }
 
-// The log of a row's sum of exp, its weights up to 2^up.  l = 0: the row saw no position.
-__device__ __forceinline__ float log_sum(float M, float l, float up = kUp) {
-  return l > 0.0f ? (M - up + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : (l == 0.0f ? -INFINITY : NAN);
+// The log of a row's sum of exp, its weights up to 2^up, and what its accumulators are multiplied by, one after the other.
+// l = 0: the row saw no position.
+struct RowSum {
+  float lse, a, b;
+};
+__device__ __forceinline__ RowSum row_sum(float M, float l, float up) {
+  const bool low = l < 0x1p-100f;  // its inverse and the logarithm want a normal number
+  const float z = low ? l * 0x1p24f : l;
+  RowSum s;
+  s.lse = l > 0.0f ? (M - up + (low ? -6.0f : 18.0f) + __builtin_amdgcn_logf(z)) * 0.69314718055994530942f
+                   : (l == 0.0f ? -INFINITY : NAN);
+  s.a = low ? 0x1p24f * kUnit : kUnit;
+  s.b = l == 0.0f ? 0.0f : 1.0f / z;
+  return s;
 }
 
 // Row r of a sequence's rows of one cache head: token-major, so that a tile's positions lie close together.
@@ -400,7 +414,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
           w[u][st / 2][0][4 * (st % 2) + i] = y16;
           if constexpr (NS == 2) w[u][st / 2][1][4 * (st % 2) + i] = (_Float16)(y - (float)y16);
         }
-      l[u] = fmaf(sum, inv, l[u]);
+      l[u] = fmaf(sum * kUnit, inv, l[u]);  // not inv * kUnit: 1 / vs may be near the least normal number
     }
     if constexpr (FMT == KM_KV_F8) {  // codes past the end may be NaN, which no weight of 0 takes out
       if (!__all(there && j0 + kChunk <= q.len)) {
@@ -466,7 +480,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
     const int r = r0 + 16 * u + m;
     if (r >= rows) continue;
     const RowAt at = row_at(A, C, q, h, r);
-    const float inv = l[u] == 0.0f ? 0.0f : 1.0f / l[u];
+    const RowSum end = row_sum(M[u], l[u], kUp);
     float *o = part + u * part_floats(NT);
     for (int n = wave; n < NT; n += W) {
       f32x4 v = sh[0].o[u * NT + n][lane];
@@ -476,7 +490,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
         *reinterpret_cast<f32x4 *>(o + (n * 64 + lane) * 4) = v;
       } else {
         const int i0 = 16 * n + 4 * g;
-        v *= inv;
+        v = v * end.a * end.b;
         const float y[4] = {v.x, v.y, v.z, v.w};
         if (i0 < d) store_o4(A, at.o + i0, y);
       }
@@ -486,7 +500,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
         o[NT * 256 + m] = M[u];
         o[NT * 256 + 16 + m] = l[u];
       } else if (A.lse) {
-        A.lse[at.lse] = log_sum(M[u], l[u]);
+        A.lse[at.lse] = end.lse;
       }
     }
   }
@@ -628,11 +642,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_join_kernel(AttendArgs P, 
   auto finish = [&](int n, const JoinSum &s) {
     if (r >= rows) return;
     const RowAt at = row_at(A, C, q, h, r);
-    const f32x4 o = s.o * (s.l == 0.0f ? 0.0f : 1.0f / s.l);
+    const RowSum end = row_sum(s.M, s.l, up);
+    const f32x4 o = s.o * end.a * end.b;
     const float y[4] = {o.x, o.y, o.z, o.w};
     const int c = G == 4 ? 16 * n + 4 * g : 32 * (n / 4) + 8 * (n % 4) + 4 * g;
     if (c < C.d) store_o4(A, at.o + c, y);
-    if (A.lse && n == 0 && g == 0) A.lse[at.lse] = log_sum(s.M, s.l, up);
+    if (A.lse && n == 0 && g == 0) A.lse[at.lse] = end.lse;
   };
   if (!spread) {
     for (int n = wave; n < NA; n += W) finish(n, sums(n, 0, 1));
@@ -1032,7 +1047,7 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
         const f16x8 a = ring[(k + KS) % RD];
         if (k + RD < KS) ring[(k + KS) % RD] = value_at(c, k + RD);
         acc[n] = mfma32(a, w[y], acc[n]);
-        if (n == 0) l = fmaf(sum[y], inv[y % NR], l);
+        if (n == 0) l = fmaf(sum[y] * kUnit, inv[y % NR], l);
         // the widening, a piece at a time
         const int p0 = k * (KP + VP) / KS, p1 = (k + 1) * (KP + VP) / KS;
 #pragma unroll
@@ -1078,17 +1093,18 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
     return;
   }
   const RowAt at = row_at(A, C, q, h, r);
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const RowSum end = row_sum(M, l, kUp32);
 #pragma unroll
   for (int n = 0; n < ND; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int c = 32 * n + 8 * i + 4 * g;
-      const float z[4] = {acc[n][4 * i] * inv, acc[n][4 * i + 1] * inv, acc[n][4 * i + 2] * inv,
-                          acc[n][4 * i + 3] * inv};
+      float z[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) z[y] = acc[n][4 * i + y] * end.a * end.b;
       if (c < d) store_o4(A, at.o + c, z);
     }
-  if (A.lse && g == 0) A.lse[at.lse] = log_sum(M, l, kUp32);
+  if (A.lse && g == 0) A.lse[at.lse] = end.lse;
 }
 
 struct Plan {

@@ -608,3 +608,128 @@ def test_one_table_row_for_all_sequences():
             res.append([*km.kv_read(s.cache, seqs), *km.kv_attend(s.cache, seqs, q, lse=True)])
         for a, b in zip(*res):
             assert torch.equal(a, b)
+
+
+def _rows64(cache, table, lens, starts, q, scale, picks):
+    """(out, lse, sum p |v|, largest scale * sum |q||k|, largest p_j times the largest value of page j) of causal rows `picks`,
+    in 64 bits from the cache's own codes and scales; one entry per (row, query head)."""
+    torch = torch_cuda()
+    heads, page, d = cache.heads, cache.page, cache.d
+    group = q.shape[1] // heads
+    qmax = 127.0 if cache.k.dtype == torch.int8 else 448.0
+    res = [[] for _ in range(5)]
+    for r in picks:
+        b = int(np.searchsorted(starts, r, side="right")) - 1
+        pos = torch.arange(int(lens[b]) - int(starts[b + 1]) + r + 1, device="cuda")
+        pg = torch.from_numpy(table[b].astype(np.int64)).cuda()[pos // page]
+        for h in range(heads):
+            k = cache.k.view(torch.uint8)[pg, h, pos % page].view(cache.k.dtype).double() * cache.k_scale[pg, h].double()[:, None]
+            v = cache.v.view(torch.uint8)[pg, h, :, pos % page].view(cache.v.dtype).double() * cache.v_scale[pg, h].double()[:, None]
+            for x in q[r, h * group:(h + 1) * group].double():
+                z = (k * x).sum(1) * scale
+                lse = torch.logsumexp(z, 0)
+                p = torch.exp(z - lse)
+                for to, y in zip(res, ((p[:, None] * v).sum(0), lse, (p[:, None] * v.abs()).sum(0),
+                                       (k.abs() * x.abs()).sum(1).max() * scale,
+                                       (p * cache.v_scale[pg, h].double()).max() * qmax)):
+                    to.append(y.cpu().numpy())
+    return [np.stack(x) for x in res]
+
+
+def _check_rows(cache, table, lens, starts, q, type_, out, lse, picks, label, step):
+    """Rows `picks` within the bound at the head of this file; step: the last step of a weight, 2^-40 of the largest for up to
+    32 rows of a head and for fp32 rows, 2^-33 for more."""
+    scale = float(np.float32(1.0 / math.sqrt(cache.d)))
+    o, L, av, big, most = _rows64(cache, table, lens, starts, q, scale, picks)
+    got = out[picks].float().cpu().numpy().astype(np.float64).reshape(o.shape)
+    gl = lse[picks].cpu().numpy().astype(np.float64).reshape(-1)
+    N = int(max(lens))
+    e = 2.0 ** -24 * (cache.d * big + 4 * ((big + np.abs(L)) * 1.45 + 16 + 128) + 8)  # value scales of 2^-100 to 2^121
+    u_w = 2.0 ** -21 if type_ == "f32" else 2.0 ** -11
+    if type_ == "f32":
+        e = e + 2.0 ** -21 * big
+    bound = U_OUT[type_] * np.abs(o) + (u_w + 2 * (e + N * 2.0 ** -24))[:, None] * av + (N * step * most)[:, None] + 1e-30
+    bad = np.abs(got - o) - bound
+    assert bad.max() <= 0, f"{label}: off by {np.abs(got - o).flat[bad.argmax()]:.3e}, bound {bound.flat[bad.argmax()]:.3e}"
+    gap = np.abs(gl - L) - (e + (N + 4 * np.abs(L)) * 2.0 ** -24)
+    assert gap.max() <= 0, f"{label}: lse {gl[gap.argmax()]} for {L[gap.argmax()]}"
+
+
+def _written(fmt, type_, page, heads, d, lens, fill):
+    """A cache whose sequences kv_write has filled with fill(b, len) -> (k, v) [len, heads, d], and its table."""
+    torch, km = torch_cuda(), _km()
+    per = [-(-l // page) for l in lens]
+    table = np.full((len(lens), max(per)), -1, np.int32)
+    at = 0
+    for b, p in enumerate(per):
+        table[b, :p] = np.arange(at, at + p)
+        at += p
+    cache = km.kv_cache(at, heads, d, page, _fmt_dtype(torch, fmt))
+    dt = getattr(torch, DT[type_])
+    for b, ln in enumerate(lens):
+        k, v = (x.to(dt) for x in fill(b, ln))
+        seqs = km.KvSeqs(torch.from_numpy(table[b:b + 1]).cuda(), torch.tensor([ln], dtype=torch.int32, device="cuda"),
+                         None, rows=ln)
+        km.kv_write(cache, seqs, k, v)
+    return cache, table
+
+
+# Calls of each way to cut one up: type, page, heads, group, d, lens, rows
+ZEROS = {
+    "even_splits": ("bf16", 64, 2, 4, 64, [8192], 1),
+    "even_splits_long": ("bf16", 64, 1, 4, 128, [131072], 1),
+    "even_splits_rows": ("f16", 16, 1, 8, 64, [16384, 9000], 4),
+    "dealt": ("bf16", 32, 8, 2, 64, [20000, 9000, 16500, 30], 1),
+    "dealt_wide_heads": ("f16", 64, 4, 1, 192, [20000, 19000, 12000, 100], 1),
+    "unsplit": ("f32", 64, 1, 1, 64, [16500], 80),
+    "split_f32": ("f32", 64, 1, 2, 64, [16500], 1),
+    "prompt_split": ("bf16", 64, 1, 4, 64, [20000], 40),
+    "prompt_split_small_pages": ("f16", 16, 1, 4, 96, [17000], 40),
+    "prompt_unsplit": ("bf16", 64, 4, 16, 64, [20000], 1024),
+}
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("name", list(ZEROS))
+def test_attend_zero_values(name, fmt):
+    """Pages of zero values, whose scale is 2^-100: alone with equal scores, alone with the first tile's scores 6.5 in
+    base 2 below the others, before real tokens, and after them."""
+    torch, km = torch_cuda(), _km()
+    type_, page, heads, group, d, lens, rows = ZEROS[name]
+    step = 2.0 ** -33 if rows * group > 32 and type_ != "f32" else 2.0 ** -40
+    g = torch.Generator(device="cuda").manual_seed(5)
+    n = len(lens)
+    starts = np.arange(n + 1) * rows
+    q = torch.full((n * rows, heads * group, d), 0.5, device="cuda").to(getattr(torch, DT[type_]))
+    picks = sorted({0, n * rows // 2, n * rows - 1})
+
+    def real(m):
+        return [torch.randn(m, heads, d, generator=g, device="cuda") for _ in range(2)]
+
+    def equal(b, ln):
+        return torch.zeros(ln, heads, d, device="cuda"), torch.zeros(ln, heads, d, device="cuda")
+
+    def rising(b, ln):
+        k = torch.full((ln, heads, d), 6.5 * math.log(2.0) / (0.5 * math.sqrt(d)), device="cuda")
+        k[:64] = 0
+        return k, torch.zeros_like(k)
+
+    def before(b, ln):
+        m = ln * 13 // 16 // page * page
+        return [torch.cat([torch.zeros(m, heads, d, device="cuda"), x]) for x in real(ln - m)]
+
+    def after(b, ln):
+        m = ln * 3 // 16 // page * page
+        return [torch.cat([x, torch.zeros(ln - m, heads, d, device="cuda")]) for x in real(m)]
+
+    for what in (equal, rising, before, after):
+        say(f"kv_attend zero values {name} {fmt} {what.__name__}")
+        cache, table = _written(fmt, type_, page, heads, d, lens, what)
+        seqs = km.KvSeqs(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), None,
+                         rows=n * rows)
+        out, lse = km.kv_attend(cache, seqs, q, lse=True)
+        torch.cuda.synchronize()
+        if what in (equal, rising):
+            assert bool((out == 0).all())
+        assert bool(torch.isfinite(lse).all())
+        _check_rows(cache, table, lens, starts, q, type_, out, lse, picks, f"{name} {what.__name__}", step)
