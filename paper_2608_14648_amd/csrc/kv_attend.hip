@@ -58,6 +58,16 @@ __device__ __forceinline__ float sum_groups(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// What brings l and the accumulators from maximum M to Mn: h * h, and where that is below the least normal number l, multiplied
+// twice, keeps its size.  A page of tiny values adds up to 2^100 times its weight to l.
+__device__ __forceinline__ float half_step(float M, float Mn) { return __builtin_amdgcn_exp2f(0.5f * (M - Mn)); }
+
+// A lane's largest weight in a chunk is 2^(t - M + up), without its page's scale 2^(z - M + up).  True: the weights are below
+// what fp16 holds and run into the least normal number, but over their page's scale they may count in l (zero pages beside
+// values of 2^48 and more), so what they add is taken from the scores alone, down to the least number there is.
+__device__ __forceinline__ bool far_below(float t, float z, float M) { return t < M - 100.0f && z > M - 146.0f; }
+__device__ __forceinline__ float far_add(float l, float x) { return fmaf(__builtin_amdgcn_exp2f(x + 24.0f), 0x1p-24f, l); }
+
 // Floats of one (tile, split) block of partial results: NT x 4 accumulators of 64 lanes per 16 rows, then M and l of
 // the 16 rows.
 __host__ __device__ constexpr int part_floats(int nt) { return nt * 256 + 32; }
@@ -394,13 +404,21 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
         for (int i = 0; i < 4; ++i) top = fmaxf(top, s[u][st][i]);
       // a factor of 0 (a row of tiny queries) would make NaN of -inf
       const float ck = fmaxf(cs[u] * k1, 0x1p-126f);
-      const float Mn = fmaxf(M[u], max_groups(fmaf(top, ck, lv)));
-      if (__any(Mn > M[u])) {
-        const float al = Mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(M[u] - Mn);
-        l[u] *= al;
+      const float tl = fmaf(top, ck, lv), Mn = fmaxf(M[u], max_groups(tl));
+      float iu = inv;
+      if (__any(Mn > M[u] || far_below(tl, tl - lv, M[u]))) {  // one branch for both: neither is common
+        const float al = Mn == -INFINITY ? 1.0f : half_step(M[u], Mn);
+        l[u] = l[u] * al * al;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[u][n] *= al;
+        for (int n = 0; n < NT; ++n) acc[u][n] *= al * al;
         M[u] = Mn;
+        if (far_below(tl, tl - lv, Mn)) {
+          iu = 0.0f;
+#pragma unroll
+          for (int st = 0; st < 4; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l[u] = far_add(l[u], fmaf(s[u][st][i], ck, kUp - 18.0f - Mn));
+        }
       }
       const float base = lv - (Mn == -INFINITY ? 0.0f : Mn) + kUp;
       float sum = 0.0f;
@@ -414,7 +432,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
           w[u][st / 2][0][4 * (st % 2) + i] = y16;
           if constexpr (NS == 2) w[u][st / 2][1][4 * (st % 2) + i] = (_Float16)(y - (float)y16);
         }
-      l[u] = fmaf(sum * kUnit, inv, l[u]);  // not inv * kUnit: 1 / vs may be near the least normal number
+      l[u] = fmaf(sum * kUnit, iu, l[u]);  // not inv * kUnit: 1 / vs may be near the least normal number
     }
     if constexpr (FMT == KM_KV_F8) {  // codes past the end may be NaN, which no weight of 0 takes out
       if (!__all(there && j0 + kChunk <= q.len)) {
@@ -466,11 +484,12 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
 #pragma unroll
     for (int y = 0; y < W; ++y) {
       const float My = sh[y].m[u][m];  // -inf: the wave has nothing
-      sum += My == -INFINITY ? 0.0f : sh[y].l[u][m] * __builtin_amdgcn_exp2f(My - Mx);
+      const float al = My == -INFINITY ? 0.0f : half_step(My, Mx);
+      sum += sh[y].l[u][m] * al * al;
     }
-    const float al = M[u] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M[u] - Mx);
+    const float al = M[u] == -INFINITY ? 0.0f : half_step(M[u], Mx);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) sh[wave].o[u * NT + n][lane] = acc[u][n] * al;
+    for (int n = 0; n < NT; ++n) sh[wave].o[u * NT + n][lane] = acc[u][n] * (al * al);
     M[u] = Mx;
     l[u] = sum;
   }
@@ -567,14 +586,14 @@ __device__ __forceinline__ void join_add(JoinSum &s, const float *My, const floa
   float M = s.M;
 #pragma unroll
   for (int i = 0; i < 4; ++i) M = fmaxf(M, My[i]);
-  const float Mu = M == -INFINITY ? 0.0f : M, a0 = __builtin_amdgcn_exp2f(s.M - Mu);
-  s.l *= a0;
-  s.o *= a0;
+  const float Mu = M == -INFINITY ? 0.0f : M, a0 = half_step(s.M, Mu);
+  s.l = s.l * a0 * a0;
+  s.o *= a0 * a0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float al = My[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(My[i] - Mu);
-    s.l = fmaf(ly[i], al, s.l);
-    s.o += oy[i] * al;
+    const float al = My[i] == -INFINITY ? 0.0f : half_step(My[i], Mu);
+    s.l = fmaf(ly[i] * al, al, s.l);
+    s.o += oy[i] * (al * al);
   }
   s.M = M;
 }
@@ -977,7 +996,7 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
         inv[y] = z.z;
         there = there && z.w != 0.0f;
       }
-      float ck[NR], base[NR], sum[4];
+      float ck[NR], base[NR], sum[4], tl[NR];
       if (!__all(there && j0 >= lo && j0 + kChunk <= hi)) {
         int jg = j0 + 8 * g;
         asm volatile("" : "+v"(jg));  // a branch: few tiles need it, so nothing of it is kept in registers
@@ -998,16 +1017,29 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
         for (int i = E * y; i < E * (y + 1); ++i) top = fmaxf(top, s[i >> 4][i & 15]);
         // a factor of 0 (a row of tiny queries) would make NaN of -inf
         ck[y] = fmaxf(cs * ks[y], 0x1p-126f);
-        Mt = fmaxf(Mt, fmaf(top, ck[y], lv[y]));
+        tl[y] = fmaf(top, ck[y], lv[y]);
+        Mt = fmaxf(Mt, tl[y]);
       }
       Mt = max_halves(Mt);
-      if (__any(Mt > M + kSlack)) {
-        const float Mn = fmaxf(M, Mt);
-        const float al = Mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(M - Mn);
-        l *= al;
+      bool rare = Mt > M + kSlack;
 #pragma unroll
-        for (int n = 0; n < ND; ++n) acc[n] *= al;
+      for (int y = 0; y < NR; ++y) rare = rare || far_below(tl[y], tl[y] - lv[y], M);
+      if (__any(rare)) {
+        const float Mn = fmaxf(M, Mt);
+        const float al = Mn == -INFINITY ? 1.0f : half_step(M, Mn);
+        l = l * al * al;
+#pragma unroll
+        for (int n = 0; n < ND; ++n) acc[n] *= al * al;
         M = Mn;
+#pragma unroll
+        for (int y = 0; y < NR; ++y) {
+          constexpr int E = 32 / NR;
+          if (!far_below(tl[y], tl[y] - lv[y], M)) continue;
+          inv[y] = 0.0f;
+#pragma unroll
+          for (int i = E * y; i < E * (y + 1); ++i)
+            l = far_add(l, fmaf(s[i >> 4][i & 15], ck[y], kUp32 - 18.0f - M));
+        }
       }
       const float up = kUp32 - (M == -INFINITY ? 0.0f : M);
 #pragma unroll

@@ -733,3 +733,45 @@ def test_attend_zero_values(name, fmt):
             assert bool((out == 0).all())
         assert bool(torch.isfinite(lse).all())
         _check_rows(cache, table, lens, starts, q, type_, out, lse, picks, f"{name} {what.__name__}", step)
+
+
+FAR = {
+    "even_splits": ("bf16", 16, 2, 2, 64, [1500], 1),
+    "dealt": ("bf16", 64, 8, 4, 64, [2100, 900, 4200, 64, 4100] * 6, 1),
+    "eight_waves": ("bf16", 64, 4, 4, 128, [2000, 640], 1),
+    "two_row_tiles": ("bf16", 32, 1, 8, 128, [700, 333], 4),
+    "f32": ("f32", 16, 1, 2, 64, [1200], 5),
+    "prompt": ("bf16", 64, 1, 4, 64, [1000, 200], 40),
+    "prompt_small_pages": ("bf16", 16, 1, 4, 128, [900], 64),
+    "prompt_wide": ("bf16", 32, 1, 2, 256, [500], 64),
+}
+
+
+@pytest.mark.parametrize("order", ["large_first", "zeros_first", "mixed"])
+@pytest.mark.parametrize("name", list(FAR))
+def test_attend_large_values_beside_zero_pages(name, order):
+    """Values of 2^60 and, in fp32 and bf16 terms, nearly the largest there are, beside zero pages whose scores are 30 above,
+    which then hold nearly all of the weight, or as high."""
+    torch, km = torch_cuda(), _km()
+    type_, page, heads, group, d, lens, rows = FAR[name]
+    step = 2.0 ** -33 if rows * group > 32 and type_ != "f32" else 2.0 ** -40
+    g = torch.Generator(device="cuda").manual_seed(6)
+    n = len(lens)
+    starts = np.arange(n + 1) * rows
+    q = torch.full((n * rows, heads * group, d), 0.5, device="cuda").to(getattr(torch, DT[type_]))
+    picks = sorted({0, n * rows // 3, n * rows - 1})
+    for size, gap in ((2.0 ** 60, 30.0), (2.0 ** 124, 30.0), (2.0 ** 126, 0.0)):
+        def fill(b, ln):
+            t = torch.arange(ln, device="cuda") // page
+            half = (ln // 2) // page
+            large = {"large_first": t < half, "zeros_first": t >= half, "mixed": t % 3 == 1}[order][:, None, None]
+            k = torch.randn(ln, heads, d, generator=g, device="cuda") * 0.05
+            v = torch.rand(ln, heads, d, generator=g, device="cuda") * size
+            return torch.where(large, k, k + gap / (0.5 * math.sqrt(d))), torch.where(large, v, torch.zeros_like(v))
+        say(f"kv_attend large values {name} {order} {size} {gap}")
+        cache, table = _written("int8", type_, page, heads, d, lens, fill)
+        seqs = km.KvSeqs(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), None,
+                         rows=n * rows)
+        out, lse = km.kv_attend(cache, seqs, q, lse=True)
+        torch.cuda.synchronize()
+        _check_rows(cache, table, lens, starts, q, type_, out, lse, picks, f"{name} {order} {size} {gap}", step)
