@@ -108,10 +108,11 @@ __device__ __forceinline__ void store_o4(const KvAttend &A, int64_t o, const flo
 }
 
 // The power of two that takes a row whose largest magnitude is top to [2^13, 2^14), and what the products of the scaled
-// row are multiplied by.  Exponents stay where the inverse is a normal number too.
+// row are multiplied by.  Exponents stay where the inverse is a normal number too.  A row with an infinity has no finite score,
+// and a softmax over those is NaN; its products could all be -infinity, which counts as not seen, so it becomes NaN here.
 __device__ __forceinline__ void q_scale(float top, float scale, float *f, float *c) {
   const int up = min(max(140 - (int)(__float_as_uint(top) >> 23), -126), 126);
-  *f = __uint_as_float((uint32_t)(127 + up) << 23);
+  *f = top == INFINITY ? NAN : __uint_as_float((uint32_t)(127 + up) << 23);
   *c = scale * kLog2e * __uint_as_float((uint32_t)(127 - up) << 23);
 }
 

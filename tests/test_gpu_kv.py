@@ -775,3 +775,30 @@ def test_attend_large_values_beside_zero_pages(name, order):
         out, lse = km.kv_attend(cache, seqs, q, lse=True)
         torch.cuda.synchronize()
         _check_rows(cache, table, lens, starts, q, type_, out, lse, picks, f"{name} {order} {size} {gap}", step)
+
+
+@pytest.mark.parametrize("rows", [1, 64])
+@pytest.mark.parametrize("type_", ["bf16", "f16", "f32"])
+def test_attend_infinite_queries(rows, type_):
+    """A query with an infinity has no finite score: NaN, also where all of its scores are -inf.  A row that sees nothing stays
+    zeros and -inf, and the other rows keep their bits."""
+    torch, km = torch_cuda(), _km()
+    d, page, lens = 64, 16, [90, 100, 1]
+    s = Setup("int8", page, 1, d, lens, [rows] * 3, seed=47)
+    s.cache.k.view(torch.int8).fill_(3)  # every product with an infinity has its sign
+    q = s.normal((s.rows, 4, d), type_)
+    good, gl = km.kv_attend(s.cache, s.seqs, q, lse=True)
+    for sign in (1.0, -1.0):
+        bad = q.clone()
+        bad[0, 1, 5] = sign * math.inf
+        bad[rows, 2, 6] = sign * math.inf
+        bad[rows, 3] = sign * math.inf
+        bad[2 * rows, 0, 0] = sign * math.inf  # before position 0 where there is more than one row
+        got, lse = km.kv_attend(s.cache, s.seqs, bad, lse=True)
+        touched = torch.zeros(q.shape[:2], dtype=torch.bool, device="cuda")
+        touched[0, 1] = touched[rows, 2] = touched[rows, 3] = touched[2 * rows, 0] = True
+        assert torch.equal(got[~touched], good[~touched]) and torch.equal(lse[~touched], gl[~touched])
+        for r, h in ((0, 1), (rows, 2), (rows, 3)) + (((2 * rows, 0),) if rows == 1 else ()):
+            assert bool(torch.isnan(got[r, h]).all()) and bool(torch.isnan(lse[r, h])), (sign, r, h)
+        if rows > 1:
+            assert bool((got[2 * rows, 0] == 0).all()) and lse[2 * rows, 0].item() == -math.inf
