@@ -137,6 +137,10 @@ __device__ __forceinline__ void kv_store(void *p, int64_t o, const float *x) {
   }
 }
 
+// The most workgroups of one launch: a grid has fewer than 2^32 threads.  What takes more is launched in pieces, of multiples of
+// eight so that each keeps the others' order over the XCDs.
+static inline int64_t kv_piece(int threads) { return (int64_t)(0xffffffffu / (unsigned)threads) & ~(int64_t)7; }
+
 // kv_cache.hip
 int64_t kv_move_blocks(const KvCache &C, const KvSeqs &S);
 km_status launch_kv_write(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v, int type, hipStream_t s);

@@ -43,6 +43,7 @@ struct AttendArgs {
   int splits;   // the most that a tile is split into; if dealt out, workgroups
   int per;      // chunks of a split or, at least, of a workgroup
   float *part;  // blocks of accumulators, then M and l: [tile][split], or if dealt out two for each workgroup
+  uint32_t block0;  // the launch's first workgroup (kv_piece); 0 if dealt out
 };
 
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
@@ -533,9 +534,10 @@ __global__ __launch_bounds__(64 * W, NT <= 8 ? 2 : 1) void kv_attend_kernel(Atte
   KvSeq q;
   if (!P.deal) {  // a workgroup per tile and split
     const uint32_t splits = max(P.splits, 1);
-    uint32_t x = blockIdx.x / splits;
-    const int split = (int)(blockIdx.x - x * splits);
-    float *part = P.part + (int64_t)blockIdx.x * RT * part_floats(NT);
+    const uint32_t block = P.block0 + blockIdx.x;
+    uint32_t x = block / splits;
+    const int split = (int)(block - x * splits);
+    float *part = P.part + (int64_t)block * RT * part_floats(NT);
     const int rt = (int)(x % (uint32_t)P.rtiles);
     x /= (uint32_t)P.rtiles;
     const int h = (int)(x % (uint32_t)P.C.heads), b = (int)(x / (uint32_t)P.C.heads);
@@ -772,7 +774,7 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   // which see the most positions, the sequences' side by side where these are about as long, else one sequence after the
   // other (four pieces of prompts of 256 dims: of equal lengths 480 us, one after the other 525; ending at 2.1 to 4.8
   // thousand positions 660 side by side, 482 one after the other).
-  uint32_t x = blockIdx.x;
+  uint32_t x = P.block0 + blockIdx.x;
   const int h = (int)(x % (uint32_t)C.heads);
   x /= (uint32_t)C.heads;
   const int split = (int)(x % (uint32_t)P.splits);
@@ -1237,14 +1239,19 @@ size_t kv_attend_scratch(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
 
 km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A, void *ws, hipStream_t s) {
   const Plan p = plan(C, S, A);
-  AttendArgs P{C, S, A, p.rtiles, p.deal, p.splits, p.per, static_cast<float *>(ws)};
-  const dim3 grid((unsigned)(p.deal ? p.splits : p.tiles * p.splits));
+  AttendArgs P{C, S, A, p.rtiles, p.deal, p.splits, p.per, static_cast<float *>(ws), 0};
+  auto go = [&](auto *kernel, int waves) {
+    const int64_t blocks = p.deal ? p.splits : p.tiles * p.splits, most = kv_piece(64 * waves);
+    for (int64_t b = 0; b < blocks; b += most) {
+      P.block0 = (uint32_t)b;
+      kernel<<<dim3((unsigned)std::min(most, blocks - b)), 64 * waves, 0, s>>>(P);
+    }
+  };
+  // Calls of 1024 tiles and more are not split up: a join is one launch.
 #define KV_J(NA, G, D, UP) \
   kv_join_kernel<NA, G, D><<<dim3((unsigned)join_blocks(p)), 64 * kJoinWaves, 0, s>>>(P, p.rt, p.spread, UP)
   if (p.prompt) {
-#define KV_K(F, N)                                                                         \
-  C.page >= kChunk ? kv_prompt_kernel<F, N, true><<<grid, 64 * kWaves, 0, s>>>(P) \
-                   : kv_prompt_kernel<F, N, false><<<grid, 64 * kWaves, 0, s>>>(P)
+#define KV_K(F, N) C.page >= kChunk ? go(kv_prompt_kernel<F, N, true>, kWaves) : go(kv_prompt_kernel<F, N, false>, kWaves)
 #define KV_N(N)                                                                                                 \
   case N:                                                                                                       \
     if (C.fmt == KM_KV_I8) KV_K(KM_KV_I8, N);                                                                   \
@@ -1265,9 +1272,8 @@ km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A,
     KMQ_LAUNCH_CHECK("kv_attend");
     return KM_OK;
   }
-#define KV_K(F, N, R, Z, W)                                                              \
-  C.page >= kChunk ? kv_attend_kernel<F, N, R, Z, true, W><<<grid, 64 * (W), 0, s>>>(P) \
-                   : kv_attend_kernel<F, N, R, Z, false, W><<<grid, 64 * (W), 0, s>>>(P)
+#define KV_K(F, N, R, Z, W) \
+  C.page >= kChunk ? go(kv_attend_kernel<F, N, R, Z, true, W>, W) : go(kv_attend_kernel<F, N, R, Z, false, W>, W)
 #define KV_W(F, N, R)                                                       \
   if (N <= 8 && p.wide) KV_K(F, N, R, 1, (N <= 8 ? kWideWaves : kAttendWaves)); \
   else KV_K(F, N, R, 1, kAttendWaves);

@@ -202,13 +202,14 @@ __device__ __forceinline__ void turn4(const uint32_t *a, uint32_t *o) {
 __device__ __forceinline__ int turn_ld(int d) { return d + 4; }
 
 template <int FMT, int TYPE>
-__global__ __launch_bounds__(1024) void kv_write_kernel(KvCache C, KvSeqs S, KvRows kr, KvRows vr, int touched) {
+__global__ __launch_bounds__(1024) void kv_write_kernel(KvCache C, KvSeqs S, KvRows kr, KvRows vr, int touched,
+                                                        uint32_t block0) {
   extern __shared__ uint32_t turn[];  // values: codes of the new rows, [token][turn_ld]
   __shared__ uint32_t sh[16];
   bool values;
   int h;
   PageJob j;
-  if (!page_job(C, S, blockIdx.x, touched, &values, &h, &j) || j.i1 == 0 || j.pg < 0) return;
+  if (!page_job(C, S, block0 + blockIdx.x, touched, &values, &h, &j) || j.i1 == 0 || j.pg < 0) return;
   const KvRows &src = values ? vr : kr;
   const int d = C.d, t = threadIdx.x, T = blockDim.x;
   const int per = d / 8, rows = j.i1 - j.i0;  // items of 8 dims in a row
@@ -361,11 +362,12 @@ __device__ __forceinline__ float value(float code, float s) {
 }
 
 template <int FMT, int TYPE>
-__global__ __launch_bounds__(1024) void kv_read_kernel(KvCache C, KvSeqs S, KvRows kr, KvRows vr, int touched) {
+__global__ __launch_bounds__(1024) void kv_read_kernel(KvCache C, KvSeqs S, KvRows kr, KvRows vr, int touched,
+                                                       uint32_t block0) {
   bool values;
   int h;
   PageJob j;
-  if (!page_job(C, S, blockIdx.x, touched, &values, &h, &j)) return;
+  if (!page_job(C, S, block0 + blockIdx.x, touched, &values, &h, &j)) return;
   const KvRows &out = values ? vr : kr;
   const int d = C.d, t = threadIdx.x, T = blockDim.x;
   for (int i = t; i < j.lead * (d / 4); i += T) {
@@ -458,8 +460,11 @@ int64_t kv_move_blocks(const KvCache &C, const KvSeqs &S) {
 km_status launch_kv_write(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v, int type, hipStream_t s) {
   const int touched = touched_pages(C, S);
   const size_t lds = (size_t)std::min(C.page, S.max_rows) * (C.d + 4);
-  const dim3 grid((unsigned)kv_move_blocks(C, S));
-#define KV_GO(F, T) kv_write_kernel<F, T><<<grid, move_threads(C, S), lds, s>>>(C, S, k, v, touched)
+  const int threads = move_threads(C, S);
+  const int64_t blocks = kv_move_blocks(C, S), most = kv_piece(threads);
+#define KV_GO(F, T)                                       \
+  for (int64_t b = 0; b < blocks; b += most)              \
+  kv_write_kernel<F, T><<<dim3((unsigned)std::min(most, blocks - b)), threads, lds, s>>>(C, S, k, v, touched, (uint32_t)b)
   if (C.fmt == KM_KV_I8) {
     if (type == KM_T_F32) KV_GO(KM_KV_I8, KM_T_F32);
     else if (type == KM_T_BF16) KV_GO(KM_KV_I8, KM_T_BF16);
@@ -476,8 +481,11 @@ km_status launch_kv_write(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v,
 
 km_status launch_kv_read(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v, int type, hipStream_t s) {
   const int touched = touched_pages(C, S);
-  const dim3 grid((unsigned)kv_move_blocks(C, S));
-#define KV_GO(F, T) kv_read_kernel<F, T><<<grid, move_threads(C, S), 0, s>>>(C, S, k, v, touched)
+  const int threads = move_threads(C, S);
+  const int64_t blocks = kv_move_blocks(C, S), most = kv_piece(threads);
+#define KV_GO(F, T)                                       \
+  for (int64_t b = 0; b < blocks; b += most)              \
+  kv_read_kernel<F, T><<<dim3((unsigned)std::min(most, blocks - b)), threads, 0, s>>>(C, S, k, v, touched, (uint32_t)b)
   if (C.fmt == KM_KV_I8) {
     if (type == KM_T_F32) KV_GO(KM_KV_I8, KM_T_F32);
     else if (type == KM_T_BF16) KV_GO(KM_KV_I8, KM_T_BF16);

@@ -802,3 +802,29 @@ def test_attend_infinite_queries(rows, type_):
             assert bool(torch.isnan(got[r, h]).all()) and bool(torch.isnan(lse[r, h])), (sign, r, h)
         if rows > 1:
             assert bool((got[2 * rows, 0] == 0).all()) and lse[2 * rows, 0].item() == -math.inf
+
+
+def test_grids_of_more_than_2_to_the_32_threads():
+    """512 sequences whose call has room for 131072 rows each: right, in several launches, as with the 256 rows that they have."""
+    torch, km = torch_cuda(), _km()
+    n, rows, heads, group, d, page = 512, 256, 8, 4, 128, 64
+    per = rows // page
+    table = torch.full((n, 131072 // page), -1, dtype=torch.int32, device="cuda")
+    table[:, :per] = torch.arange(n * per, device="cuda").view(n, per)
+    lens = torch.full((n,), rows, dtype=torch.int32, device="cuda")
+    starts = torch.arange(n + 1, dtype=torch.int32, device="cuda") * rows
+    assert n * (131072 // page) * 2 * heads * 256 >= 2 ** 32  # kv_write's and kv_read's threads
+    assert n * heads * (n * rows * group // 128) * 256 >= 2 ** 32  # kv_attend's
+    g = torch.Generator(device="cuda").manual_seed(8)
+    k = torch.randn(n * rows, heads, d, generator=g, device="cuda").bfloat16()
+    q = torch.randn(n * rows, heads * group, d, generator=g, device="cuda").bfloat16()
+    res = []
+    for most in (None, rows):
+        say(f"kv_write, kv_read, kv_attend with max_rows {most}")
+        cache = km.kv_cache(n * per, heads, d, page)
+        seqs = km.KvSeqs(table, lens, starts, rows=n * rows, max_rows=most)
+        km.kv_write(cache, seqs, k, k)
+        res.append([cache.k, cache.v, *km.kv_read(cache, seqs), *km.kv_attend(cache, seqs, q, lse=True)])
+        torch.cuda.synchronize()
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
