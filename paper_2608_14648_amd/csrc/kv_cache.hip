@@ -370,9 +370,10 @@ __global__ __launch_bounds__(1024) void kv_read_kernel(KvCache C, KvSeqs S, KvRo
   if (!page_job(C, S, block0 + blockIdx.x, touched, &values, &h, &j)) return;
   const KvRows &out = values ? vr : kr;
   const int d = C.d, t = threadIdx.x, T = blockDim.x;
-  for (int i = t; i < j.lead * (d / 4); i += T) {
+  // by rows: there may be more values than 32 bits count
+  for (Place p = {t / (d / 4), t % (d / 4)}; p.r < j.lead; advance(p, d / 4, T / (d / 4), T % (d / 4))) {
     const float z[4] = {0, 0, 0, 0};
-    kv_store<TYPE, 4>(out.p, (j.row0 + i / (d / 4)) * out.row + h * out.head + i % (d / 4) * 4, z);
+    kv_store<TYPE, 4>(out.p, (j.row0 + p.r) * out.row + h * out.head + p.c * 4, z);
   }
   if (j.i1 == 0) return;
   const int64_t at = j.row * out.row + h * out.head;

@@ -828,3 +828,22 @@ def test_grids_of_more_than_2_to_the_32_threads():
         torch.cuda.synchronize()
     for a, b in zip(*res):
         assert torch.equal(a, b)
+
+
+def test_read_many_rows_before_the_start():
+    """2^25 rows and more before position 0, 256 dims: zeros, counted in 64 bits."""
+    torch, km = torch_cuda(), _km()
+    rows, d = (1 << 25) + 70, 256
+    cache = km.kv_cache(1, 1, d, 16)
+    cache.k.fill_(1)
+    cache.v.fill_(2)
+    seqs = km.KvSeqs(torch.zeros((1, 1), dtype=torch.int32, device="cuda"),
+                     torch.tensor([3], dtype=torch.int32, device="cuda"), None, rows=rows)
+    k = torch.full((rows, 1, d), 7.0, dtype=torch.float16, device="cuda")
+    v = torch.full((rows, 1, d), 7.0, dtype=torch.float16, device="cuda")
+    km.kv_read(cache, seqs, k=k, v=v)
+    torch.cuda.synchronize()
+    for x, code in ((k, 1.0), (v, 2.0)):
+        assert bool((x[-3:] == code).all())
+        for part in x[:-3].split(1 << 22):
+            assert not bool(part.any())
