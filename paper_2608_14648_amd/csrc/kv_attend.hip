@@ -1172,7 +1172,7 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   p.rtiles = (int)cdiv(rows, (p.prompt ? 32 : 16) * p.rt);
   p.tiles = (int64_t)S.n * C.heads * p.rtiles;
   if (p.prompt) {
-    p.per = (int)std::max<int64_t>(8, cdiv(p.tiles * chunks, 512));
+    p.per = (int)std::min(chunks, std::max<int64_t>(8, cdiv(p.tiles * chunks, 512)));
     p.spread = p.tiles * p.rt < 256;
   } else {
     // Short contexts, or tiles enough to fill the card several times: a workgroup for each tile and no join.  A

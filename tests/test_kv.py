@@ -204,3 +204,14 @@ def test_table_rows_of_one_address_or_apart(kmq):
         assert km.KvSeqs(table(1, 5, 0), lens[:1])._c.table_ld == 5
     c, s, _ = (ct.byref(x) for x in _args(kmq, seqs=dict(table_ld=0)))
     assert kmq.lib().kv_attend_bytes(c, s, 4, 1, 0, 1) == 0
+
+
+@needs_lib
+def test_plan_of_the_largest_calls(kmq):
+    """Tables of 2^30 positions with many row tiles: the chunks of all tiles pass 2^40 and their share per workgroup 2^31."""
+    L = kmq.lib()
+    for heads, n, rows in ((8, 128, 8192), (8, 128, 8191), (8, 100, 20000), (1, 2000, 70000)):
+        c, s, _ = (ct.byref(x) for x in _args(kmq, dict(heads=heads), dict(n=n, max_pages=1 << 24, table_ld=1 << 24,
+                                                                           max_rows=rows, rows=n * rows)))
+        # tiles enough for the whole card: none is split, no workspace
+        assert L.kv_attend_bytes(c, s, 2 * heads, 1, 0, 1) == 0, L.km_last_error().decode()
