@@ -20,6 +20,11 @@ _raw_stream = torch._C._cuda_getCurrentRawStream  # the handle alone: current_st
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
+def _beside(t: torch.Tensor, name: str, other: torch.Tensor):
+    if t.device != other.device:
+        raise ValueError(f"{name} must be on {other.device} (got {t.device})")
+
+
 class KvCache:
     """Codes and scales of a paged cache (mirrors ``km_kv_cache``).
 
@@ -31,11 +36,13 @@ class KvCache:
             raise TypeError(f"k must be int8 or float8_e4m3fn (got {k.dtype})")
         _dev(k, k.dtype, "k", 4)
         _dev(v, k.dtype, "v", 4)
+        _beside(v, "v", k)
         pages, heads, page, d = k.shape
         if tuple(v.shape) != (pages, heads, d, page):
             raise ValueError("v must be [pages, heads, d, page] for k [pages, heads, page, d]")
         for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             _dev(t, torch.float32, name, 2)
+            _beside(t, name, k)
             if tuple(t.shape) != (pages, heads):
                 raise ValueError(f"{name} must be [pages, heads]")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
@@ -72,6 +79,7 @@ class KvSeqs:
                 table.dim() != 2 or table.shape[1] < 1 or table.stride(1) != 1:
             raise ValueError("table must be a 2-D int32 tensor on the GPU with contiguous rows")
         _dev(lens, torch.int32, "lens", 1)
+        _beside(lens, "lens", table)
         n = table.shape[0]
         if lens.shape[0] != n:
             raise ValueError("lens must hold one length per row of table")
@@ -79,6 +87,7 @@ class KvSeqs:
             rows = n
         if starts is not None:
             _dev(starts, torch.int32, "starts", 1)
+            _beside(starts, "starts", table)
             if starts.shape[0] != n + 1:
                 raise ValueError("starts must hold n + 1 values")
             max_rows = rows if max_rows is None else max_rows

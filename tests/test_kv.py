@@ -215,3 +215,32 @@ def test_plan_of_the_largest_calls(kmq):
                                                                            max_rows=rows, rows=n * rows)))
         # tiles enough for the whole card: none is split, no workspace
         assert L.kv_attend_bytes(c, s, 2 * heads, 1, 0, 1) == 0, L.km_last_error().decode()
+
+
+@needs_lib
+def test_binding_refuses_tensors_of_several_devices():
+    """Every tensor of a cache and of the sequences is on one GPU.  (Fake tensors: no memory, so two GPUs are not needed.)"""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    import paper_2608_14648_amd as km
+    with FakeTensorMode():
+        def codes(dev):
+            return torch.empty((2, 1, 16, 16), dtype=torch.int8, device=dev)
+
+        def scales(dev):
+            return torch.empty((2, 1), device=dev)
+
+        def ints(n, dev):
+            return torch.empty(n, dtype=torch.int32, device=dev)
+
+        a, b = "cuda:0", "cuda:1"
+        km.KvCache(codes(a), codes(a), scales(a), scales(a))
+        for devs, name in (((a, b, a, a), "v"), ((a, a, b, a), "k_scale"), ((b, b, b, a), "v_scale")):
+            with pytest.raises(ValueError, match=f"^{name} must be on"):
+                km.KvCache(codes(devs[0]), codes(devs[1]), scales(devs[2]), scales(devs[3]))
+        table = torch.empty((3, 4), dtype=torch.int32, device=a)
+        km.KvSeqs(table, ints(3, a), ints(4, a), rows=9)
+        with pytest.raises(ValueError, match="^lens must be on"):
+            km.KvSeqs(table, ints(3, b))
+        with pytest.raises(ValueError, match="^starts must be on"):
+            km.KvSeqs(table, ints(3, a), ints(4, b), rows=9)
