@@ -3,6 +3,8 @@
 A KvCache is four tensors that the caller owns; a KvSeqs says which rows of a call belong to which sequence.  Both keep the
 descriptors that the C ABI takes, so a program that serves makes them once (a KvSeqs once per step, for all layers) and a
 call costs little more than its launch.
+
+The cache serves and nothing is trained through it: rows that require grad are refused unless gradients are off.
 """
 from __future__ import annotations
 
@@ -116,6 +118,9 @@ def _rows_of(t: torch.Tensor, name: str, seqs: KvSeqs, heads: int, d: int, dtype
         raise TypeError(f"{name} must be {dtype or 'float32, bfloat16 or float16'} (got {t.dtype})")
     if t.device != seqs.device:
         raise ValueError(f"{name} must be on {seqs.device} (got {t.device})")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires grad, and nothing is passed back through the cache: call under torch.no_grad() or "
+                         "detach it")
     if t.shape != (seqs.rows, heads, d):
         raise ValueError(f"{name} must be [{seqs.rows}, {heads}, {d}] (got {tuple(t.shape)})")
     row, head, one = t.stride()

@@ -244,3 +244,30 @@ def test_binding_refuses_tensors_of_several_devices():
             km.KvSeqs(table, ints(3, b))
         with pytest.raises(ValueError, match="^starts must be on"):
             km.KvSeqs(table, ints(3, a), ints(4, b), rows=9)
+
+
+@needs_lib
+def test_binding_refuses_rows_that_require_grad():
+    """No result without its graph: refused while gradients are recorded, taken where they are off.  (Fake tensors; without rows
+    there is nothing to launch.)"""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    import paper_2608_14648_amd as km
+    with FakeTensorMode():
+        dev = "cuda:0"
+        codes, scales = torch.empty((2, 1, 16, 16), dtype=torch.int8, device=dev), torch.empty((2, 1), device=dev)
+        cache = km.KvCache(codes, codes, scales, scales)
+        none = torch.empty(0, dtype=torch.int32, device=dev)
+        seqs = km.KvSeqs(torch.empty((0, 1), dtype=torch.int32, device=dev), none)
+        x = torch.empty((0, 1, 16), device=dev)
+        g = torch.empty((0, 1, 16), device=dev, requires_grad=True)
+        calls = [lambda t: km.kv_write(cache, seqs, t, x), lambda t: km.kv_write(cache, seqs, x, t),
+                 lambda t: km.kv_read(cache, seqs, k=t, v=x), lambda t: km.kv_attend(cache, seqs, t),
+                 lambda t: km.kv_attend(cache, seqs, x, out=t)]
+        for call in calls:
+            with pytest.raises(ValueError, match="requires grad"):
+                call(g)
+            call(x)
+            call(g.detach())
+            with torch.no_grad():
+                call(g)
