@@ -1235,7 +1235,7 @@ static km_status check_attend(const KvCache &c, const KvSeqs &s, int32_t q_heads
   o->type = type;
   o->group = q_heads / c.heads;
   o->causal = flags & KM_KV_CAUSAL;
-  o->window = window;
+  o->window = std::min(window, 1 << 30);  // sees all that a sequence can have; first positions then stay within 32 bits
   KMQ_CHECK((int64_t)s.max_rows * o->group < (1 << 30), KM_EINVAL, "max_rows * q_heads / heads = %lld must be < 2^30",
             (long long)s.max_rows * o->group);
   return s.n ? check_grid(kv_attend_blocks(c, s, *o)) : KM_OK;

@@ -847,3 +847,16 @@ def test_read_many_rows_before_the_start():
         assert bool((x[-3:] == code).all())
         for part in x[:-3].split(1 << 22):
             assert not bool(part.any())
+
+
+@pytest.mark.parametrize("type_,rows", [("bf16", 3), ("bf16", 40), ("f32", 20)])
+def test_attend_windows_of_any_size(type_, rows):
+    """A window that no sequence fills changes nothing, up to the largest number, with rows before position 0 in the same tiles."""
+    torch, km = torch_cuda(), _km()
+    s = Setup("int8", 16, 1, 64, [rows - 2 if rows < 4 else 9, 200], [rows + 3, rows], seed=53)
+    q = s.normal((s.rows, 4, 64), type_)
+    want = km.kv_attend(s.cache, s.seqs, q, lse=True)
+    assert bool((want[1][:rows + 3] == -math.inf).any()) and bool((want[1][:rows + 3] > -math.inf).any())
+    for window in (2 ** 31 - 1, 2 ** 30, 2 ** 30 - 1, 1000):
+        got = km.kv_attend(s.cache, s.seqs, q, window=window, lse=True)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), window
