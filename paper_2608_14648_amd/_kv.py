@@ -22,6 +22,11 @@ _raw_stream = torch._C._cuda_getCurrentRawStream  # the handle alone: current_st
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
+def _i32(x: int) -> int:
+    """A number as the C ABI takes it: one past 32 bits is the largest or -1, not its low half."""
+    return max(-1, min(x, 2 ** 31 - 1))
+
+
 def _beside(t: torch.Tensor, name: str, other: torch.Tensor):
     if t.device != other.device:
         raise ValueError(f"{name} must be on {other.device} (got {t.device})")
@@ -107,7 +112,7 @@ class KvSeqs:
         self.n, self.rows, self.max_rows, self.max_len = n, rows, max_rows, max_len
         self.device = table.device
         self._c = KmKvSeqs(n, table.shape[1], table.data_ptr(), ld, lens.data_ptr(),
-                           None if starts is None else starts.data_ptr(), rows, max_rows, max_len)
+                           None if starts is None else starts.data_ptr(), rows, _i32(max_rows), _i32(max_len))
         self._ref = ct.addressof(self._c)
 
 
@@ -190,6 +195,7 @@ def kv_attend(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, scale: float | None
         return out, L
     flags = KM_KV_CAUSAL if causal else 0
     t = _TYPES[q.dtype]
+    window = _i32(window)
     lb = lib()
     need = lb.kv_attend_bytes(cache._ref, seqs._ref, q_heads, flags, window, t)
     if need < 0:

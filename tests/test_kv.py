@@ -271,3 +271,37 @@ def test_binding_refuses_rows_that_require_grad():
             call(g.detach())
             with torch.no_grad():
                 call(g)
+
+
+@needs_lib
+def test_binding_does_not_wrap_numbers():
+    """max_rows, max_len and window past 32 bits: the largest number or a refusal, not their low halves."""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    import paper_2608_14648_amd as km
+    from paper_2608_14648_amd import _kv
+    seen = []
+
+    class Lib:
+        def kv_attend_bytes(self, cache, seqs, q_heads, flags, window, type_):
+            seen.append(window)
+            return -1
+
+        def km_last_error(self):
+            return b"seen"
+
+    with FakeTensorMode():
+        dev = "cuda:0"
+        codes, scales = torch.empty((2, 1, 16, 16), dtype=torch.int8, device=dev), torch.empty((2, 1), device=dev)
+        cache = km.KvCache(codes, codes, scales, scales)
+        table = torch.empty((2, 4), dtype=torch.int32, device=dev)
+        lens, starts = (torch.empty(n, dtype=torch.int32, device=dev) for n in (2, 3))
+        top = 2 ** 31 - 1
+        for given, held in ((2 ** 32 + 1, top), (2 ** 31, top), (top, top), (7, 7), (-2 ** 32 + 5, -1)):
+            s = km.KvSeqs(table, lens, starts, rows=5, max_rows=given, max_len=given)
+            assert (s._c.max_rows, s._c.max_len) == (held, held)
+            with pytest.MonkeyPatch.context() as m:
+                m.setattr(_kv, "lib", Lib)
+                with pytest.raises(km.KmqError, match="seen"):
+                    km.kv_attend(cache, s, torch.empty((5, 1, 16), device=dev), window=given)
+            assert seen[-1] == held
