@@ -860,3 +860,33 @@ def test_attend_windows_of_any_size(type_, rows, first):
     for window in (2 ** 31 - 1, 2 ** 30, 2 ** 30 - 1, 1000):
         got = km.kv_attend(s.cache, s.seqs, q, window=window, lse=True)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), window
+
+
+@pytest.mark.parametrize("n", [64, 65, 70])
+def test_attend_prompts_of_many_sequences(n):
+    """Prompts of differing lengths, up to 64 sequences ordered by length and more as they come."""
+    lens = _ragged(n, 90, 13)
+    s = Setup("int8", 16, 1, 64, lens, [min(x, 12) for x in lens], seed=59)
+    _attend_check(s, s.normal((s.rows, 4, 64), "bf16", 0.4), "bf16", label=f"{n} prompts")
+
+
+@pytest.mark.parametrize("rows,below,step", [(64, 26, 2.0 ** -33), (1, 33, 2.0 ** -40)])
+def test_attend_weights_of_few_bits(rows, below, step):
+    """Half of the pages have value scales 2^-below of the others', whose codes are 0 in the upper dims: results there are made of
+    weights near fp16's last step, which is 2^-32 of the largest weight for more than 32 rows and 2^-39 for fewer."""
+    torch, km = torch_cuda(), _km()
+    d, page, n = 64, 16, 400
+    per = n // page
+    g = torch.Generator(device="cuda").manual_seed(9)
+    k, v = (torch.randint(-127, 128, s, generator=g, device="cuda", dtype=torch.int8) for s in ((per, 1, page, d), (per, 1, d, page)))
+    v[::2, :, d // 2:] = 0
+    vs = torch.ones((per, 1), device="cuda")
+    vs[1::2] = 2.0 ** -below
+    cache = km.KvCache(k, v, torch.full((per, 1), 2.0 ** -8, device="cuda"), vs)
+    table, lens = np.arange(per, dtype=np.int32)[None], [n]
+    seqs = km.KvSeqs(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"), None, rows=rows)
+    q = torch.randn(rows, 1, d, generator=g, device="cuda").bfloat16()
+    out, lse = km.kv_attend(cache, seqs, q, lse=True)
+    torch.cuda.synchronize()
+    assert bool((out[:, :, d // 2:].abs() < 2.0 ** (7 - below)).all()) and bool((out[:, :, d // 2:] != 0).any())
+    _check_rows(cache, table, lens, np.array([0, rows]), q, "bf16", out, lse, list(range(0, rows, 9)), f"{rows} rows", step)
