@@ -486,7 +486,8 @@ km_status kv_read(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_
  *   positions j of the sequence that the row sees: j <= its own with KM_KV_CAUSAL, and with window > 0 (then
  *   KM_KV_CAUSAL is needed) the last `window` of these.  Positions on pages that are not there are not seen.
  *   q, out: rows of q_heads heads of the type; lse (nullable): float[rows][q_heads], log sum_j exp(scale <q, k_j>).
- *   A row that sees no position gets zeros and -infinity, one with a NaN or an infinity among its queries NaN.
+ *   A row that sees no position gets zeros and -infinity, one with a NaN or an infinity among its queries NaN, and so does
+ *   one with a score * log2(e) of 2^128 or more (scores below -2^128 count as not seen).
  *   q_heads: a multiple of heads; max_rows * q_heads / heads < 2^30.  scale: finite, > 0.
  *   ws (nullable): kv_attend_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the
  *   pool.  Codes of positions inside a sequence have to be finite and their pages' scales finite and not below 2^-100

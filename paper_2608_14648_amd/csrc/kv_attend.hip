@@ -1110,6 +1110,7 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   }
 
   l += __shfl_xor(l, 32);
+  if (M == INFINITY) l = NAN;  // scores past fp32's range: no weight is left to tell them from a row that sees nothing
   const int r = rw + m;
   if (r >= rows) return;
   if (splits > 1) {

@@ -890,3 +890,21 @@ def test_attend_weights_of_few_bits(rows, below, step):
     torch.cuda.synchronize()
     assert bool((out[:, :, d // 2:].abs() < 2.0 ** (7 - below)).all()) and bool((out[:, :, d // 2:] != 0).any())
     _check_rows(cache, table, lens, np.array([0, rows]), q, "bf16", out, lse, list(range(0, rows, 9)), f"{rows} rows", step)
+
+
+@pytest.mark.parametrize("rows", [1, 64, 2048])
+@pytest.mark.parametrize("type_", ["bf16", "f32"])
+def test_attend_scores_past_fp32(rows, type_):
+    """Finite queries whose scores are past fp32's range: NaN as from any other sum in 32 bits, not zeros, in every kernel; the
+    other rows keep their bits."""
+    torch, km = torch_cuda(), _km()
+    s = Setup("int8", 64, 1, 64, [rows + 90], [rows], seed=61)
+    s.cache.k.view(torch.int8).fill_(100)
+    q = s.normal((s.rows, 4, 64), type_)
+    good, gl = km.kv_attend(s.cache, s.seqs, q, lse=True)
+    bad = q.clone()
+    bad[rows // 2, 1] = 3e38
+    got, lse = km.kv_attend(s.cache, s.seqs, bad, lse=True)
+    assert bool(torch.isnan(got[rows // 2, 1]).all()) and bool(torch.isnan(lse[rows // 2, 1]))
+    got[rows // 2, 1], lse[rows // 2, 1] = good[rows // 2, 1], gl[rows // 2, 1]
+    assert torch.equal(got, good) and torch.equal(lse, gl)
