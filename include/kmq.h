@@ -488,7 +488,8 @@ km_status kv_read(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_
  *   q, out: rows of q_heads heads of the type; lse (nullable): float[rows][q_heads], log sum_j exp(scale <q, k_j>).
  *   A row that sees no position gets zeros and -infinity, one with a NaN or an infinity among its queries NaN, and so does
  *   one with a score * log2(e) of 2^128 or more (scores below -2^128 count as not seen).
- *   q_heads: a multiple of heads; max_rows * q_heads / heads < 2^30.  scale: finite, > 0.
+ *   q_heads: a multiple of heads; max_rows * q_heads / heads < 2^30; fp32: max_rows * q_heads < 2^28 (whole row tiles).
+ *   scale: finite, > 0.
  *   ws (nullable): kv_attend_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the
  *   pool.  Codes of positions inside a sequence have to be finite and their pages' scales finite and not below 2^-100
  *   (kv_write makes no others); what lies behind its end is not looked at.

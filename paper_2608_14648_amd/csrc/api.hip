@@ -1238,7 +1238,10 @@ static km_status check_attend(const KvCache &c, const KvSeqs &s, int32_t q_heads
   o->window = std::min(window, 1 << 30);  // sees all that a sequence can have; first positions then stay within 32 bits
   KMQ_CHECK((int64_t)s.max_rows * o->group < (1 << 30), KM_EINVAL, "max_rows * q_heads / heads = %lld must be < 2^30",
             (long long)s.max_rows * o->group);
-  return s.n ? check_grid(kv_attend_blocks(c, s, *o)) : KM_OK;
+  if (s.n == 0) return KM_OK;
+  KMQ_CHECK(kv_attend_fits(c, s, *o), KM_EINVAL, "max_rows * q_heads = %lld: fp32 rows of one sequence must be < 2^28",
+            (long long)s.max_rows * q_heads);
+  return check_grid(kv_attend_blocks(c, s, *o));
 }
 
 }  // namespace kmq

@@ -157,6 +157,8 @@ struct KvAttend {
   float *lse;    // nullable, [rows][heads * group]
 };
 size_t kv_attend_scratch(const KvCache &C, const KvSeqs &S, const KvAttend &A);
+// Whether one sequence of the call fits a launch (16-bit rows always do).
+bool kv_attend_fits(const KvCache &C, const KvSeqs &S, const KvAttend &A);
 int64_t kv_attend_blocks(const KvCache &C, const KvSeqs &S, const KvAttend &A);
 km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A, void *ws, hipStream_t s);
 

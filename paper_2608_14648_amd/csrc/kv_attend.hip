@@ -43,7 +43,7 @@ struct AttendArgs {
   int splits;   // the most that a tile is split into; if dealt out, workgroups
   int per;      // chunks of a split or, at least, of a workgroup
   float *part;  // blocks of accumulators, then M and l: [tile][split], or if dealt out two for each workgroup
-  uint32_t block0;  // the launch's first workgroup (kv_piece); 0 if dealt out
+  uint32_t block0;  // the launch's first workgroup (kv_prompt_kernel; see kv_piece)
 };
 
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
@@ -534,10 +534,9 @@ __global__ __launch_bounds__(64 * W, NT <= 8 ? 2 : 1) void kv_attend_kernel(Atte
   KvSeq q;
   if (!P.deal) {  // a workgroup per tile and split
     const uint32_t splits = max(P.splits, 1);
-    const uint32_t block = P.block0 + blockIdx.x;
-    uint32_t x = block / splits;
-    const int split = (int)(block - x * splits);
-    float *part = P.part + (int64_t)block * RT * part_floats(NT);
+    uint32_t x = blockIdx.x / splits;
+    const int split = (int)(blockIdx.x - x * splits);
+    float *part = P.part + (int64_t)blockIdx.x * RT * part_floats(NT);
     const int rt = (int)(x % (uint32_t)P.rtiles);
     x /= (uint32_t)P.rtiles;
     const int h = (int)(x % (uint32_t)P.C.heads), b = (int)(x / (uint32_t)P.C.heads);
@@ -1226,6 +1225,11 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
 static int accumulators(const Plan &p) { return p.nt * (p.prompt ? 4 : 1); }
 static int64_t join_blocks(const Plan &p) { return p.tiles * p.rt * (p.spread ? accumulators(p) : 1); }
 
+bool kv_attend_fits(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
+  const Plan p = plan(C, S, A);  // workgroups of eight waves are for few tiles
+  return p.prompt || p.tiles / S.n <= kv_piece(64 * kAttendWaves);
+}
+
 int64_t kv_attend_blocks(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   const Plan p = plan(C, S, A);
   return std::max(p.tiles * (p.deal ? 1 : p.splits), join_blocks(p));
@@ -1241,18 +1245,38 @@ size_t kv_attend_scratch(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
 km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A, void *ws, hipStream_t s) {
   const Plan p = plan(C, S, A);
   AttendArgs P{C, S, A, p.rtiles, p.deal, p.splits, p.per, static_cast<float *>(ws), 0};
-  auto go = [&](auto *kernel, int waves) {
-    const int64_t blocks = p.deal ? p.splits : p.tiles * p.splits, most = kv_piece(64 * waves);
+  auto go_prompt = [&](auto *kernel) {
+    const int64_t blocks = p.tiles * p.splits, most = kv_piece(64 * kWaves);
     for (int64_t b = 0; b < blocks; b += most) {
       P.block0 = (uint32_t)b;
-      kernel<<<dim3((unsigned)std::min(most, blocks - b)), 64 * waves, 0, s>>>(P);
+      kernel<<<dim3((unsigned)std::min(most, blocks - b)), 64 * kWaves, 0, s>>>(P);
     }
   };
-  // Calls of 1024 tiles and more are not split up: a join is one launch.
+  // In pieces of whole sequences where it takes some: an offset in the kernel costs single tokens 2 %.
+  auto go = [&](auto *kernel, int waves) {
+    const int64_t each = p.deal ? p.splits : p.tiles / S.n * p.splits, most = p.deal ? S.n : kv_piece(64 * waves) / each;
+    for (int64_t b = 0; b < S.n; b += most) {
+      AttendArgs Q = P;
+      Q.S.n = (int)std::min(most, S.n - b);
+      Q.S.table += b * S.table_ld;
+      Q.S.lens += b;
+      if (S.starts) {
+        Q.S.starts += b;
+      } else if (b) {
+        const int64_t row = b * S.max_rows, elem = A.type == KM_T_F32 ? 4 : 2;
+        Q.S.rows -= row;
+        Q.A.q.p = static_cast<char *>(A.q.p) + row * A.q.row * elem;
+        Q.A.out.p = static_cast<char *>(A.out.p) + row * A.out.row * elem;
+        if (A.lse) Q.A.lse += row * C.heads * A.group;
+      }
+      kernel<<<dim3((unsigned)(p.deal ? each : Q.S.n * each)), 64 * waves, 0, s>>>(Q);
+    }
+  };
+  // Calls of 1024 tiles and more are not split up: their pieces have no joins, and a join is one launch.
 #define KV_J(NA, G, D, UP) \
   kv_join_kernel<NA, G, D><<<dim3((unsigned)join_blocks(p)), 64 * kJoinWaves, 0, s>>>(P, p.rt, p.spread, UP)
   if (p.prompt) {
-#define KV_K(F, N) C.page >= kChunk ? go(kv_prompt_kernel<F, N, true>, kWaves) : go(kv_prompt_kernel<F, N, false>, kWaves)
+#define KV_K(F, N) C.page >= kChunk ? go_prompt(kv_prompt_kernel<F, N, true>) : go_prompt(kv_prompt_kernel<F, N, false>)
 #define KV_N(N)                                                                                                 \
   case N:                                                                                                       \
     if (C.fmt == KM_KV_I8) KV_K(KM_KV_I8, N);                                                                   \

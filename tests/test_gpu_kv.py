@@ -908,3 +908,24 @@ def test_attend_scores_past_fp32(rows, type_):
     assert bool(torch.isnan(got[rows // 2, 1]).all()) and bool(torch.isnan(lse[rows // 2, 1]))
     got[rows // 2, 1], lse[rows // 2, 1] = good[rows // 2, 1], gl[rows // 2, 1]
     assert torch.equal(got, good) and torch.equal(lse, gl)
+
+
+def test_attend_more_single_tokens_than_one_grid_takes():
+    """131077 sequences of 128 heads in one call, a workgroup each: as the same in three calls, with and without row ranges."""
+    torch, km = torch_cuda(), _km()
+    n, heads, d = (1 << 17) + 5, 128, 16
+    assert n * heads * 256 >= 2 ** 32
+    g = torch.Generator(device="cuda").manual_seed(10)
+    k, v = (torch.randint(-127, 128, (1, heads, 16, 16), generator=g, device="cuda", dtype=torch.int8) for _ in range(2))
+    cache = km.KvCache(k, v, *(torch.full((1, heads), 0.05, device="cuda") for _ in range(2)))
+    table = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    lens = torch.randint(0, 17, (n,), generator=g, device="cuda", dtype=torch.int32)
+    q = torch.randn(n, heads, d, generator=g, device="cuda", dtype=torch.bfloat16)
+    starts = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    parts = [km.kv_attend(cache, km.KvSeqs(table.expand(b - a, -1), lens[a:b].clone()), q[a:b], lse=True)
+             for a, b in ((0, 50000), (50000, 100001), (100001, n))]
+    want = [torch.cat(x) for x in zip(*parts)]
+    for st in (None, starts):
+        out = torch.full_like(q, 3.0)
+        _, lse = km.kv_attend(cache, km.KvSeqs(table.expand(n, -1), lens, st, rows=n, max_rows=1), q, out=out, lse=True)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])

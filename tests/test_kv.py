@@ -305,3 +305,15 @@ def test_binding_does_not_wrap_numbers():
                 with pytest.raises(km.KmqError, match="seen"):
                     km.kv_attend(cache, s, torch.empty((5, 1, 16), device=dev), window=given)
             assert seen[-1] == held
+
+
+@needs_lib
+def test_one_sequence_of_more_rows_than_a_grid_takes(kmq):
+    """fp32 rows of one sequence, 2^28 of them over the query heads and more, are refused; bf16 ones are launched in pieces."""
+    L = kmq.lib()
+    for rows, status in (((1 << 24) - 1024, 0), (1 << 24, -1)):
+        c, s, _ = (ct.byref(x) for x in _args(kmq, dict(heads=8), dict(n=1, max_pages=1 << 20, table_ld=1 << 20, max_rows=rows,
+                                                                     rows=rows)))
+        assert L.kv_attend_bytes(c, s, 16, 1, 0, 1) == 0
+        assert L.kv_attend_bytes(c, s, 16, 1, 0, 0) == status
+    assert "max_rows" in L.km_last_error().decode()
