@@ -10,8 +10,11 @@
 //
 // q'_i is the row times the power of two that brings its largest value to [2^13, 2^14): a 16-bit value stays exact down
 // to 2^-27 of the row's largest.  Taking the maximum of the weight with its value scale keeps w in fp16's range for
-// whatever scales the pages have; w is rounded to fp16 (2^-12 relative, down to 2^-29 of the largest weight) for
-// the second product, l and every sum are fp32.  fp32 queries take two halves of q' and of w and twice the products.
+// whatever scales the pages have; w is rounded to fp16 for the second product (at most 2^-11 relative, down to 2^-29 of the largest
+// weight, below that steps of 2^-39 of it; where the maximum lags, in kv_prompt_kernel, 2^-22 and 2^-32), l and every sum are
+// fp32.  The rounding leaves fp16 results 2.4e-4 to 2.9e-4 from the exact ones (root mean square, relative; their own rounding
+// alone 2.1e-4), bf16 ones where they are; a second half of w would take half as many products again.  fp32 queries take two
+// halves of q' and of w and twice the products.
 //
 // Layout.  One wave takes 64 positions and 16 rows at a time, without LDS.  The scores are computed transposed (keys are
 // the matrix instruction's rows, queries its columns), and the keys of the four 16-key products are chosen so that lane
@@ -19,9 +22,10 @@
 // product, whose other operand is 16 contiguous bytes of one dim of the value page.  A page is 16 tokens or more, so
 // a lane's 16 positions share one page and its scales.
 //
-// Measured (8 cache heads of 128, bf16): one sequence of 131071 tokens 45 us for 268 MB and 5 to join; 64 sequences of 1 to
-// 16384 tokens 179 us for 1028 MB, 5.7 TB/s, where a read alone reaches 6.3.  A chunk of a wave is about 520 vector
-// instructions, 320 of them the widening of int8 codes (five per four codes, e4m3 two), and 32 products.
+// Measured (8 cache heads of 128, bf16): one sequence of 131071 tokens 45 us for 268 MB and 4 to join; 64 sequences of 1 to
+// 16384 tokens 176 us for 1028 MB, 5.8 TB/s, where a read alone reaches 6.3.  A chunk of a wave is about 540 vector
+// instructions, 320 of them the widening of int8 codes (five per four codes, e4m3 two), and 32 products.  16 rows of 128 dims take 208
+// registers, two waves to a SIMD; 32 rows take all 256 and spill 8 to 14 (36 to 60 bytes of scratch).
 #include "kv.hpp"
 
 namespace kmq {
@@ -713,10 +717,10 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_join_kernel(AttendArgs P, 
 // are loaded one tile before they are widened.
 //
 // Measured (prompt of 16384, 32 query heads of 128 on 8): 2.3 ms, 950 TFLOP/s, where a large fp16 library product reaches
-// 1310 on this card (both run into its power limit, about 1.9 GHz).  The matrix cores are busy for 44 % of the time, the
-// vector unit for 59 %, LDS for 40 %.  Two waves to a SIMD.  Tried: 64 rows to a wave, one wave to a SIMD (halves the LDS
+// 1310 on this card (both run into its power limit, about 1.9 GHz).  The matrix cores are busy for 43 % of the time, the
+// vector unit for 60 %, LDS for 40 %.  Two waves to a SIMD.  Tried: 64 rows to a wave, one wave to a SIMD (halves the LDS
 // reads, 3.3 ms); eight waves to a workgroup (halves the widening, no change).  Heads of more than 128 dims leave a SIMD
-// one wave only, and its phases in turn: 390 TFLOP/s at 256.
+// one wave only, and its phases in turn: 390 TFLOP/s at 256 (pages below 64 also spill up to 10 registers there).
 
 constexpr float kUp32 = 8.0f, kSlack = 7.0f;
 
@@ -1179,20 +1183,25 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
     // workgroup takes 6.5 us and 1.7 more per 256 positions (8 heads of 128); splitting it up and joining takes 14 us up to
     // some 4096 positions, more where tiles nearly fill the card by themselves: pieces of them are then short, and there are
     // many to join.  Where a workgroup per tile leaves every workgroup little to do, even splits; where it streams for long,
-    // what differing lengths leave idle counts for more, and tiles are dealt out.  8 heads of 128, lengths from 1 on:
+    // what differing lengths leave idle counts for more, and tiles are dealt out.  8 heads of 128 in bf16, the size that the
+    // bounds below are from, lengths from 1 on:
     //   64 sequences up to 16384 (512 tiles): 194 us dealt out, 225 even splits; up to 4000: 56, a workgroup each 61
     //   256 up to 4000 (2048 tiles): 242 us dealt out, 213 a workgroup each; 128 up to 4000: 130 either way
     //   31 up to 3000 (248 tiles): 37 us dealt out, 27 a workgroup each; 31 of 6000 91 and 71; 24 up to 8000: 47 and 52
     //   16 up to 1500 (128 tiles): 19 us even splits, 15 a workgroup each; up to 3000: 23 and 25
     //   8 up to 1500 (64 tiles): 14 us even splits, 15 a workgroup each
     //   16 behind a window of 4096, 4 heads (64 tiles): 39 us dealt out, 28 even splits
+    // Workgroups of four waves (wider heads, fp32) gain less from a workgroup each, up to 3000 positions: 31 of fp32 up to 3000 33 us
+    // so, 40 dealt out, 24 up to 6000 55 and 47; 31 of 256 dims up to 3000 52 and 70, 24 up to 6000 97 and 94.
     // Workgroups of eight waves (accumulators of up to 128 dims, 16-bit types) have the loads of a CU in flight with half the
     // tiles' beginnings, ends and pieces to join, but wait for each other at both:
     //   a tile each, 32 up to 2000: 23.2 us with four waves, 20.8 with eight; one of 300 7.0 and 7.2 (64 dims)
     //   even splits, one head, 100000 positions: 22.7 and 17.9; one sequence of 1500, 8 heads: 11.3 and 12.9
     //   dealt out, 64 up to 16384: 194 and 187; 32 up to 8000: 48 and 51; 2 up to 29000 of 16 heads (32 tiles): 26 and 27;
     //   32 rows to a tile, 64 up to 4000: 68 and 104
-    // As many workgroups as run at a time.
+    // Narrower heads keep four waves: dealt out, 64 up to 16384 of 64 dims 111 us with four and 118 with eight, of 80 139 and 144,
+    // of 96 162 and 160; even splits are alike, but for one head, 100000 positions: 20 and 15.
+    // Workgroups that run at a time with 128 dims, two waves to a SIMD (64 dims have room for three or four).
     const int64_t cap = (int64_t)S.max_pages * C.page / kChunk + 1 + kTileCost;  // whatever max_len says
     const int64_t most = p.nt <= 8 ? 512 : 256;
     const bool eight = p.nt <= 8 && A.type != KM_T_F32;

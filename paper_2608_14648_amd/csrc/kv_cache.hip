@@ -7,7 +7,7 @@
 // their codes turn through LDS on the way in and in registers on the way out.
 //
 // Both are bound by HBM: 3 bytes per 16-bit element, 4.6 and 5.7 TB/s for 74631 tokens of 8 heads of 128 (100 and 80 us;
-// a large copy 4.7).  One token: 3.1 and 3.7 us.  The rows of a page are read once and kept in registers (a
+// a large copy 4.7); fp32 rows, 82674 tokens, 5.6 and 4.1 TB/s (152 and 207 us).  One token: 3.1 and 3.7 us.  The rows of a page are read once and kept in registers (a
 // workgroup has as many threads as that takes), its largest magnitude is taken on the bit patterns, and only a page that
 // holds infinities or NaN looks at them one by one.
 #include "kv.hpp"
