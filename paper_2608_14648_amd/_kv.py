@@ -85,7 +85,7 @@ class KvSeqs:
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, starts: torch.Tensor | None = None,
                  rows: int | None = None, max_rows: int | None = None, max_len: int = 0):
         if not isinstance(table, torch.Tensor) or table.device.type != "cuda" or table.dtype != torch.int32 or \
-                table.dim() != 2 or table.shape[1] < 1 or table.stride(1) != 1:
+                table.dim() != 2 or table.shape[1] < 1 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table must be a 2-D int32 tensor on the GPU with contiguous rows")
         _dev(lens, torch.int32, "lens", 1)
         _beside(lens, "lens", table)

@@ -317,3 +317,17 @@ def test_one_sequence_of_more_rows_than_a_grid_takes(kmq):
         assert L.kv_attend_bytes(c, s, 16, 1, 0, 1) == 0
         assert L.kv_attend_bytes(c, s, 16, 1, 0, 0) == status
     assert "max_rows" in L.km_last_error().decode()
+
+
+@needs_lib
+def test_table_of_one_page_has_any_column_stride():
+    """The stride of an axis of one is of no meaning: a row of pages turned into a table of one page each is taken."""
+    import torch
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    import paper_2608_14648_amd as km
+    with FakeTensorMode():
+        lens = torch.empty(5, dtype=torch.int32, device="cuda:0")
+        table = torch.empty((1, 5), dtype=torch.int32, device="cuda:0").t()
+        assert table.stride() == (1, 5) and km.KvSeqs(table, lens)._c.table_ld == 1
+        with pytest.raises(ValueError, match="contiguous rows"):
+            km.KvSeqs(torch.empty((2, 5), dtype=torch.int32, device="cuda:0").t(), lens)
