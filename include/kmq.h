@@ -393,15 +393,16 @@ km_status kmeans_fit_hier(const km_points *P, int32_t k, const km_hier_params *h
 km_status kmeans_cost(const float *X, int64_t n, int32_t d, int64_t ldx, const float *C, int32_t k,
                       const int32_t *assign, double *out, km_stream stream);
 
-/* ---- Key/value cache in 8 bits ----------------------------------------------------------------------------------
+/* ---- Key/value cache in 8 and 4 bits ----------------------------------------------------------------------------
  *
  * Keys and values of a transformer's past tokens as 8-bit codes in pages (blocks of `page` tokens), one scale per
- * page and head, and the attention that reads them.  A sequence's position p is token p % page of page
- * table[p / page].
+ * page and head, or as 4-bit codes with one scale per token and head, and the attention that reads them.  A sequence's
+ * position p is token p % page of page table[p / page].
  */
 typedef enum {
   KM_KV_I8 = 0, /* whole numbers -127 .. 127 */
-  KM_KV_F8 = 1  /* e4m3 (OCP, no infinities, largest 448) */
+  KM_KV_F8 = 1, /* e4m3 (OCP, no infinities, largest 448) */
+  KM_KV_I4 = 4  /* whole numbers -7 .. 7, held as code + 8, two to a byte, the even dim or token in the low half */
 } km_kv_format;
 
 typedef enum { KM_T_F32 = 0, KM_T_BF16 = 1, KM_T_F16 = 2 } km_type; /* rows given to and taken from the cache */
@@ -411,6 +412,8 @@ typedef enum { KM_T_F32 = 0, KM_T_BF16 = 1, KM_T_F16 = 2 } km_type; /* rows give
  *   page: 16, 32, 64 or 128 tokens.  d: 16 .. 256, d % 16 == 0.  1 <= pages < 2^31.  heads * page * d < 2^31.
  *   k: codes [pages][heads][page][d]; v: codes [pages][heads][d][page] (dims first: the attention sums over
  *   tokens).  k_scale, v_scale: float[pages][heads].  k and v 16-byte aligned.  A new cache needs no contents.
+ *   I4: d % 32 == 0; k: bytes [pages][heads][page][d / 2]; v: bytes [pages][heads][d][page / 2]; k_scale, v_scale:
+ *   float[pages][heads][page].
  */
 typedef struct km_kv_cache {
   int32_t fmt; /* km_kv_format */
@@ -466,6 +469,8 @@ typedef struct km_kv_rows {
  * A 16-bit x times mul is exact in fp32, and fp32 rows are rounded as the exact product is, so codes do not depend on how
  * the product is computed.  A call that writes a page's first token gives it a new scale.  Rows that fall before position 0
  * or on a page that is not there are skipped.  No two sequences of a call may write the same page.
+ *   I4: the same for each row (the d values of a token and head) by itself, with qmax = 7 and mul within [2^-30, 2^30]; codes
+ *   past -7 and 7 (a > 7 * 2^30) are -7 and 7.  No earlier code changes.
  */
 km_status kv_write(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *k, const km_kv_rows *v,
                    int32_t type, km_stream stream);
@@ -491,8 +496,8 @@ km_status kv_read(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_
  *   q_heads: a multiple of heads; max_rows * q_heads / heads < 2^30; fp32: max_rows * q_heads < 2^28 (whole row tiles).
  *   scale: finite, > 0.
  *   ws (nullable): kv_attend_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the
- *   pool.  Codes of positions inside a sequence have to be finite and their pages' scales finite and not below 2^-100
- *   (kv_write makes no others); what lies behind its end is not looked at.
+ *   pool.  Codes of positions inside a sequence have to be finite and their pages' scales finite and not below 2^-100,
+ *   I4: their scales within [2^-30, 2^30] (kv_write makes no others); what lies behind its end is not looked at.
  *   fp32 queries: products and weights in two halves each (about 22 bits); 16-bit ones: their own bits, weights rounded to
  *   fp16; sums, maxima and normalisation in fp32.
  *   The result does not depend on scheduling.
@@ -504,6 +509,75 @@ km_status kv_attend(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_k
 /* Bytes of ws that kv_attend uses for these arguments (0: none; < 0: a km_status). */
 int64_t kv_attend_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t q_heads, int32_t flags,
                         int32_t window, int32_t type);
+
+/* ---- Around the cache: positions and eviction ------------------------------------------------------------------- */
+
+/*
+ * Rotary positions.  dims (even, 2 .. d) of every head are turned, the rest stays.  layout: pair i of a head is dims i and
+ * i + dims / 2 (KM_ROT_HALVES) or 2 i and 2 i + 1 (KM_ROT_PAIRS).  freq: DEVICE double[dims / 2], radians per position of
+ * each pair.  amplitude: finite, sine and cosine are multiplied by it.
+ */
+typedef enum { KM_ROT_HALVES = 0, KM_ROT_PAIRS = 1 } km_kv_layout;
+typedef struct km_kv_rotary {
+  int32_t dims;
+  int32_t layout; /* km_kv_layout */
+  const double *freq;
+  float amplitude;
+} km_kv_rotary;
+
+/* kv_rotate() flags */
+#define KM_ROT_INVERSE 1 /* turned back; also what takes the gradient of a result to that of its input */
+
+/*
+ * kv_rotate -- queries and keys turned by their rows' positions: pair (x, y) of a row at position p becomes
+ *   amplitude (x cos pf - y sin pf, x sin pf + y cos pf), with KM_ROT_INVERSE of -pf.  The angle is taken in 64 bits, products in
+ *   fp32, results are rounded to the type once.
+ *   Positions are those of seqs (only lens, starts and the numbers of rows are looked at; rows before position 0 have negative
+ *   ones; rows of sequences that do not fit are left as they are) or, where positions is not NULL (then seqs is NULL),
+ *   positions[row], DEVICE int32[rows], any number.  rows: with positions, of q and k.
+ *   q, k: rows of q_heads and k_heads heads of d (a multiple of 16 up to 256; (q_heads + k_heads) d < 2^27) of the type; k and k_out
+ *   NULL and k_heads 0: queries alone.  q_out, k_out: the same rows as q and k (turned in place) or rows that overlap none of them.
+ */
+km_status kv_rotate(const km_kv_rotary *rotary, const km_kv_seqs *seqs, const int32_t *positions, int64_t rows,
+                    const km_kv_rows *q, int32_t q_heads, const km_kv_rows *k, int32_t k_heads, const km_kv_rows *q_out,
+                    const km_kv_rows *k_out, int32_t d, int32_t type, int32_t flags, km_stream stream);
+
+/*
+ * kv_weigh -- the attention weight that cached tokens get from the rows' queries, added to what they had:
+ *   weight[page][head][token] of every position j of the sequences = decay * what it was + sum over the rows and their query heads
+ *   of that cache head of exp(scale <q, k_j> - lse), over the rows that see j (as in kv_attend).  The call's own positions (the
+ *   last ones, one for each row) begin with the sum alone, and with decay = 0 nothing that was there is looked at.
+ *   lse: float[rows][q_heads] as kv_attend leaves it for these rows and this cache; a row's head whose lse is not finite adds nothing.
+ *   weight: DEVICE float[pages][heads][page].  decay: finite, >= 0.  Sums are fp32, in an order that does not depend on scheduling.
+ *   Positions on pages that are not there have no weight.  No two sequences of a call may have a page in common.
+ *   q_heads, scale, flags, window, type: as in kv_attend; max_rows * q_heads / heads < 2^30.
+ */
+km_status kv_weigh(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *q, int32_t q_heads, float scale,
+                   int32_t flags, int32_t window, int32_t type, const float *lse, float *weight, float decay,
+                   km_stream stream);
+
+/*
+ * kv_evict -- every sequence keeps keep[b] of its tokens, each head its own, and closes the gaps: the first `first` and the last
+ *   `recent` positions, then those of the largest weight, ties to the lower position (first and recent count as of infinite
+ *   weight, NaN as less than all).  The kept tokens of a head, in their order,
+ *   become its positions 0, 1, ...: codes, scales and weights move; what lies behind them stays as it is.  8-bit codes take the
+ *   smallest multiplier of the tokens that come to their page and are coded again where theirs was larger, as in kv_write; 4-bit
+ *   ones do not change.  The pages behind the last kept position are free then.
+ *   seqs: n, max_pages, table, table_ld and lens are looked at; a sequence whose length does not fit, or that has a page that is
+ *   not there, is left as it is.
+ *   weight: DEVICE float[pages][heads][page].  keep: DEVICE int32[n], of which max(0, min(keep[b], max_keep)) counts.
+ *   first, recent >= 0, first + recent <= max_keep, 1 <= max_keep <= 2^30.
+ *   kept: DEVICE int32[n][heads][max_keep], the position that each kept token had, -1 where there is none.  lens (out): DEVICE
+ *   int32[n], how many are kept (of a sequence that is left as it is: its length); not seqs->lens.
+ *   ws (nullable): kv_evict_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the pool.
+ *   No two sequences of a call may have a page in common.
+ */
+km_status kv_evict(const km_kv_cache *cache, const km_kv_seqs *seqs, float *weight, const int32_t *keep, int32_t max_keep,
+                   int32_t first, int32_t recent, int32_t *kept, int32_t *lens, void *ws, int64_t ws_bytes,
+                   km_stream stream);
+
+/* Bytes of ws that kv_evict uses for these arguments (< 0: a km_status). */
+int64_t kv_evict_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t max_keep);
 
 /* Thread-local message for the last non-OK status ("" if none). */
 const char *km_last_error(void);

@@ -18,7 +18,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libkmq.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "assign.hip", "split.hip", "split_small.hip", "update.hip", "quantize.hip", "pca.hip", "hier.hip", "skm.hip",
-           "kv_cache.hip", "kv_attend.hip"]
+           "kv_cache.hip", "kv_cache4.hip", "kv_attend.hip", "kv_attend_f8.hip", "kv_attend_i4.hip", "kv_rotate.hip", "kv_weigh.hip",
+           "kv_evict.hip"]
 ARCH = os.environ.get("KMQ_OFFLOAD_ARCH", "gfx950")
 
 CFLAGS = [

@@ -1153,10 +1153,12 @@ namespace kmq {
 
 static km_status check_cache(const km_kv_cache *c, KvCache *o) {
   KMQ_CHECK(c != nullptr, KM_EINVAL, "cache descriptor is NULL");
-  KMQ_CHECK(c->fmt == KM_KV_I8 || c->fmt == KM_KV_F8, KM_EUNSUPPORTED, "unknown cache format %d", c->fmt);
+  KMQ_CHECK(c->fmt == KM_KV_I8 || c->fmt == KM_KV_F8 || c->fmt == KM_KV_I4, KM_EUNSUPPORTED, "unknown cache format %d",
+            c->fmt);
   KMQ_CHECK(c->page == 16 || c->page == 32 || c->page == 64 || c->page == 128, KM_EINVAL,
             "page = %d must be 16, 32, 64 or 128", c->page);
   KMQ_CHECK(c->d >= 16 && c->d <= 256 && c->d % 16 == 0, KM_EINVAL, "d = %d must be a multiple of 16 up to 256", c->d);
+  KMQ_CHECK(c->fmt != KM_KV_I4 || c->d % 32 == 0, KM_EINVAL, "d = %d must be a multiple of 32 for 4-bit codes", c->d);
   KMQ_CHECK(c->heads >= 1 && (int64_t)c->heads * c->page * c->d < INT32_MAX, KM_EINVAL,
             "heads = %d must be >= 1 and heads * page * d < 2^31", c->heads);
   KMQ_CHECK(c->pages >= 1 && c->pages < (int64_t)INT32_MAX, KM_EINVAL, "pages = %lld outside [1, 2^31)",
@@ -1169,19 +1171,19 @@ static km_status check_cache(const km_kv_cache *c, KvCache *o) {
   return KM_OK;
 }
 
-// OK with o->n == 0: a call without rows
-static km_status check_seqs(const km_kv_seqs *s, const KvCache &c, KvSeqs *o) {
+// OK with o->n == 0: a call without rows, or with whole sequences (their rows are not looked at) one without sequences
+static km_status check_seqs(const km_kv_seqs *s, const KvCache &c, KvSeqs *o, bool whole = false) {
   KMQ_CHECK(s != nullptr, KM_EINVAL, "sequences descriptor is NULL");
   KMQ_CHECK(s->n >= 0 && s->rows >= 0 && s->max_rows >= 0 && s->max_len >= 0, KM_EINVAL,
             "n, rows, max_rows and max_len must be >= 0");
   *o = KvSeqs{};
-  if (s->n == 0 || s->rows == 0 || s->max_rows == 0) return KM_OK;
+  if (s->n == 0 || (!whole && (s->rows == 0 || s->max_rows == 0))) return KM_OK;
   KMQ_CHECK(s->table != nullptr && s->lens != nullptr, KM_EINVAL, "NULL argument");
   KMQ_CHECK(s->max_pages >= 1 && (s->table_ld >= s->max_pages || s->table_ld == 0), KM_EINVAL,
             "need table_ld >= max_pages >= 1 (or table_ld = 0)");
   KMQ_CHECK((int64_t)s->max_pages * c.page <= ((int64_t)1 << 30), KM_EINVAL, "max_pages * page = %lld above 2^30",
             (long long)s->max_pages * c.page);
-  KMQ_CHECK(s->starts != nullptr || s->rows == (int64_t)s->n * s->max_rows, KM_EINVAL,
+  KMQ_CHECK(whole || s->starts != nullptr || s->rows == (int64_t)s->n * s->max_rows, KM_EINVAL,
             "without starts rows must be n * max_rows");
   KMQ_CHECK(s->rows < (int64_t)INT32_MAX && s->max_rows < (1 << 30), KM_EINVAL,
             "rows = %lld outside [0, 2^31) or max_rows = %d outside [0, 2^30)", (long long)s->rows, s->max_rows);
@@ -1220,11 +1222,13 @@ static km_status kv_move(const km_kv_cache *cache, const km_kv_seqs *seqs, const
   if (st == KM_OK) st = check_grid(kv_move_blocks(c, s));
   if (st != KM_OK) return st;
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  if (c.fmt == KM_KV_I4) return write ? launch_kv_write4(c, s, kr, vr, type, hs) : launch_kv_read4(c, s, kr, vr, type, hs);
   return write ? launch_kv_write(c, s, kr, vr, type, hs) : launch_kv_read(c, s, kr, vr, type, hs);
 }
 
-static km_status check_attend(const KvCache &c, const KvSeqs &s, int32_t q_heads, int32_t flags, int32_t window,
-                              int32_t type, KvAttend *o) {
+// What the attention and the weights of its positions have in common.
+static km_status check_queries(const KvCache &c, const KvSeqs &s, int32_t q_heads, int32_t flags, int32_t window,
+                               int32_t type, KvAttend *o) {
   KMQ_CHECK(type == KM_T_F32 || type == KM_T_BF16 || type == KM_T_F16, KM_EUNSUPPORTED, "unknown type %d of rows", type);
   KMQ_CHECK(q_heads >= 1 && q_heads % c.heads == 0, KM_EINVAL, "q_heads = %d must be a multiple of heads = %d", q_heads,
             c.heads);
@@ -1238,7 +1242,13 @@ static km_status check_attend(const KvCache &c, const KvSeqs &s, int32_t q_heads
   o->window = std::min(window, 1 << 30);  // sees all that a sequence can have; first positions then stay within 32 bits
   KMQ_CHECK((int64_t)s.max_rows * o->group < (1 << 30), KM_EINVAL, "max_rows * q_heads / heads = %lld must be < 2^30",
             (long long)s.max_rows * o->group);
-  if (s.n == 0) return KM_OK;
+  return KM_OK;
+}
+
+static km_status check_attend(const KvCache &c, const KvSeqs &s, int32_t q_heads, int32_t flags, int32_t window,
+                              int32_t type, KvAttend *o) {
+  const km_status st = check_queries(c, s, q_heads, flags, window, type, o);
+  if (st != KM_OK || s.n == 0) return st;
   KMQ_CHECK(kv_attend_fits(c, s, *o), KM_EINVAL, "max_rows * q_heads = %lld: fp32 rows of one sequence must be < 2^28",
             (long long)s.max_rows * q_heads);
   return check_grid(kv_attend_blocks(c, s, *o));
@@ -1303,6 +1313,127 @@ km_status kv_attend(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_k
               (long long)need, (long long)ws_bytes);
   }
   return launch_kv_attend(c, s, a, ws, hs);
+}
+
+km_status kv_rotate(const km_kv_rotary *rotary, const km_kv_seqs *seqs, const int32_t *positions, int64_t rows,
+                    const km_kv_rows *q, int32_t q_heads, const km_kv_rows *k, int32_t k_heads, const km_kv_rows *q_out,
+                    const km_kv_rows *k_out, int32_t d, int32_t type, int32_t flags, km_stream stream) {
+  g_err[0] = 0;
+  KMQ_CHECK(rotary != nullptr, KM_EINVAL, "rotary descriptor is NULL");
+  KMQ_CHECK(d >= 16 && d <= 256 && d % 16 == 0, KM_EINVAL, "d = %d must be a multiple of 16 up to 256", d);
+  KMQ_CHECK(rotary->dims >= 2 && rotary->dims <= d && rotary->dims % 2 == 0, KM_EINVAL, "dims = %d must be even and within [2, %d]",
+            rotary->dims, d);
+  KMQ_CHECK(rotary->layout == KM_ROT_HALVES || rotary->layout == KM_ROT_PAIRS, KM_EUNSUPPORTED, "unknown layout %d",
+            rotary->layout);
+  KMQ_CHECK(rotary->freq != nullptr && reinterpret_cast<uintptr_t>(rotary->freq) % 8 == 0, KM_EINVAL,
+            "freq must not be NULL and be 8-byte aligned");
+  KMQ_CHECK(std::isfinite(rotary->amplitude), KM_EINVAL, "amplitude = %g must be finite", (double)rotary->amplitude);
+  KMQ_CHECK((flags & ~KM_ROT_INVERSE) == 0, KM_EINVAL, "unknown flags 0x%x", flags);
+  KMQ_CHECK((seqs == nullptr) != (positions == nullptr), KM_EINVAL, "either seqs or positions must be given");
+  KMQ_CHECK(q_heads >= 1 && k_heads >= 0 && ((int64_t)q_heads + k_heads) * d < (1 << 27), KM_EINVAL,
+            "q_heads = %d must be >= 1, k_heads = %d >= 0 and (q_heads + k_heads) * d < 2^27", q_heads, k_heads);
+  KvRotate r{};
+  if (positions != nullptr) {
+    KMQ_CHECK(rows >= 0 && rows < (int64_t)INT32_MAX, KM_EINVAL, "rows = %lld outside [0, 2^31)", (long long)rows);
+    if (rows == 0) return KM_OK;
+  } else {
+    KvCache c{};
+    c.page = 1;
+    km_status st = check_seqs(seqs, c, &r.S);
+    if (st != KM_OK || r.S.n == 0) return st;
+  }
+  r.positions = positions;
+  r.rows = rows;
+  km_status st = check_rows(q, type, "q", &r.q);
+  if (st == KM_OK) st = check_rows(q_out, type, "q_out", &r.q_out);
+  if (st == KM_OK && k_heads) st = check_rows(k, type, "k", &r.k);
+  if (st == KM_OK && k_heads) st = check_rows(k_out, type, "k_out", &r.k_out);
+  if (st != KM_OK) return st;
+  auto same = [](const KvRows &a, const KvRows &b) { return a.p == b.p && a.row == b.row && a.head == b.head; };
+  r.q_in_place = same(r.q, r.q_out);
+  r.k_in_place = same(r.k, r.k_out);
+  r.q_heads = q_heads;
+  r.k_heads = k_heads;
+  r.d = d;
+  r.dims = rotary->dims;
+  r.neighbours = rotary->layout == KM_ROT_PAIRS;
+  r.inverse = flags & KM_ROT_INVERSE;
+  r.freq = rotary->freq;
+  r.amplitude = rotary->amplitude;
+  st = check_grid(kv_rotate_blocks(r));
+  if (st != KM_OK) return st;
+  return launch_kv_rotate(r, type, reinterpret_cast<hipStream_t>(stream));
+}
+
+km_status kv_weigh(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *q, int32_t q_heads, float scale,
+                   int32_t flags, int32_t window, int32_t type, const float *lse, float *weight, float decay,
+                   km_stream stream) {
+  g_err[0] = 0;
+  KvCache c;
+  KvSeqs s;
+  KvAttend a;
+  km_status st = check_cache(cache, &c);
+  if (st == KM_OK) st = check_seqs(seqs, c, &s);
+  if (st == KM_OK) st = check_queries(c, s, q_heads, flags, window, type, &a);
+  if (st != KM_OK) return st;
+  KMQ_CHECK(scale > 0.0f && std::isfinite(scale), KM_EINVAL, "scale = %g must be finite and > 0", (double)scale);
+  KMQ_CHECK(decay >= 0.0f && std::isfinite(decay), KM_EINVAL, "decay = %g must be finite and >= 0", (double)decay);
+  KMQ_CHECK(s.n < 2 || s.table_ld != 0, KM_EINVAL, "sequences of one table row share their pages' weights");
+  if (s.n == 0) return KM_OK;
+  KMQ_CHECK(lse != nullptr && weight != nullptr, KM_EINVAL, "NULL argument");
+  st = check_rows(q, type, "q", &a.q);
+  if (st == KM_OK) st = check_grid(kv_weigh_blocks(c, s, a));
+  if (st != KM_OK) return st;
+  a.scale = scale;
+  a.lse = const_cast<float *>(lse);  // read only
+  return launch_kv_weigh(c, s, a, weight, decay, reinterpret_cast<hipStream_t>(stream));
+}
+
+static km_status check_evict(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t max_keep, KvCache *c, KvSeqs *s) {
+  km_status st = check_cache(cache, c);
+  if (st == KM_OK) st = check_seqs(seqs, *c, s, true);
+  if (st != KM_OK) return st;
+  KMQ_CHECK(max_keep >= 1 && max_keep <= (1 << 30), KM_EINVAL, "max_keep = %d outside [1, 2^30]", max_keep);
+  KMQ_CHECK(s->n < 2 || s->table_ld != 0, KM_EINVAL, "sequences of one table row share their pages");
+  KMQ_CHECK((int64_t)s->n * c->heads < (1 << 22), KM_EINVAL, "n * heads = %lld must be < 2^22", (long long)s->n * c->heads);
+  return s->n ? check_grid(kv_evict_blocks(*c, *s, max_keep)) : KM_OK;
+}
+
+int64_t kv_evict_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t max_keep) {
+  g_err[0] = 0;
+  KvCache c;
+  KvSeqs s;
+  const km_status st = check_evict(cache, seqs, max_keep, &c, &s);
+  if (st != KM_OK) return st;
+  return s.n ? (int64_t)kv_evict_scratch(c, s, max_keep) : 0;
+}
+
+km_status kv_evict(const km_kv_cache *cache, const km_kv_seqs *seqs, float *weight, const int32_t *keep, int32_t max_keep,
+                   int32_t first, int32_t recent, int32_t *kept, int32_t *lens, void *ws, int64_t ws_bytes,
+                   km_stream stream) {
+  g_err[0] = 0;
+  KvCache c;
+  KvSeqs s;
+  km_status st = check_evict(cache, seqs, max_keep, &c, &s);
+  if (st != KM_OK) return st;
+  KMQ_CHECK(first >= 0 && recent >= 0 && (int64_t)first + recent <= max_keep, KM_EINVAL,
+            "first = %d and recent = %d must be >= 0 and together at most max_keep = %d", first, recent, max_keep);
+  if (s.n == 0) return KM_OK;
+  KMQ_CHECK(weight != nullptr && keep != nullptr && kept != nullptr && lens != nullptr, KM_EINVAL, "NULL argument");
+  KMQ_CHECK(aligned16(weight), KM_EINVAL, "weight must be 16-byte aligned");
+  KMQ_CHECK(lens != s.lens, KM_EINVAL, "lens must not be the sequences' own");
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const int64_t need = (int64_t)kv_evict_scratch(c, s, max_keep);
+  Scratch own(hs);
+  if (ws == nullptr) {
+    st = own.alloc((size_t)need);
+    if (st != KM_OK) return st;
+    ws = own.get();
+  } else {
+    KMQ_CHECK(ws_bytes >= need && aligned16(ws), KM_EINVAL, "ws needs %lld bytes (got %lld) and 16-byte alignment",
+              (long long)need, (long long)ws_bytes);
+  }
+  return launch_kv_evict(c, s, KvEvict{weight, keep, max_keep, first, recent, kept, lens}, ws, hs);
 }
 
 }  // extern "C"

@@ -79,6 +79,15 @@ __device__ __forceinline__ float kv_mul_of_scale(float s) {
   return m > 0.0f && m <= 0x1p100f ? m : 0x1p100f;           // a scale that was never written
 }
 
+// 4-bit codes: a row's multiplier lies within [2^-30, 2^30], so that no two scales of a cache are more than 2^60 apart.
+__device__ __forceinline__ float kv_mul4_of_top(float top) {
+  return fmaxf(kv_short(fminf(7.0f / top, 0x1p30f)), 0x1p-30f);  // top = 0: 2^30
+}
+
+// Bytes of n codes.
+template <int FMT>
+__host__ __device__ constexpr int64_t kv_bytes(int64_t n) { return FMT == KM_KV_I4 ? n / 2 : n; }
+
 // Four codes of a dword, 8 bits each, as halves: both formats' values are exact in fp16.
 template <int FMT>
 __device__ __forceinline__ void kv_widen4(uint32_t c, f16x2 *lo, f16x2 *hi) {
@@ -99,6 +108,23 @@ __device__ __forceinline__ f16x8 kv_widen8(uint32_t a, uint32_t b) {
   kv_widen4<FMT>(a, x, x + 1);
   kv_widen4<FMT>(b, x + 2, x + 3);
   return f16x8{x[0].x, x[0].y, x[1].x, x[1].y, x[2].x, x[2].y, x[3].x, x[3].y};
+}
+
+// Eight 4-bit codes of a dword as halves, in the order 0 4 1 5 2 6 3 7: code + 8 in the low bits of 1024's pattern is
+// 1024 + code + 8.  kv_place4 is where code i of eight ends up: what such codes are multiplied with is laid out the same.
+__device__ __forceinline__ f16x8 kv_widen4x8(uint32_t w) {
+  const f16x2 off = {(_Float16)1032.0f, (_Float16)1032.0f};
+  f16x2 x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u) - off;
+  return f16x8{x[0].x, x[0].y, x[1].x, x[1].y, x[2].x, x[2].y, x[3].x, x[3].y};
+}
+__host__ __device__ constexpr int kv_place4(int i) { return i < 4 ? 2 * i : 2 * i - 7; }
+
+// What lane L of each sixteen holds, in all of them (all lanes have to be active).
+template <int L>
+__device__ __forceinline__ float kv_row_bcast(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x150 + L, 0xf, 0xf, false));
 }
 
 // 16-bit and 32-bit rows
@@ -141,10 +167,30 @@ __device__ __forceinline__ void kv_store(void *p, int64_t o, const float *x) {
 // eight so that each keeps the others' order over the XCDs.
 static inline int64_t kv_piece(int threads) { return (int64_t)(0xffffffffu / (unsigned)threads) & ~(int64_t)7; }
 
-// kv_cache.hip
+// kv_cache.hip, kv_cache4.hip
 int64_t kv_move_blocks(const KvCache &C, const KvSeqs &S);
 km_status launch_kv_write(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v, int type, hipStream_t s);
 km_status launch_kv_read(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v, int type, hipStream_t s);
+km_status launch_kv_write4(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v, int type, hipStream_t s);
+km_status launch_kv_read4(const KvCache &C, const KvSeqs &S, KvRows k, KvRows v, int type, hipStream_t s);
+
+// kv_rotate.hip
+struct KvRotate {
+  KvSeqs S;
+  const int32_t *positions;  // nullable: of every row, instead of S
+  int64_t rows;
+  KvRows q, k, q_out, k_out;
+  int q_heads, k_heads;  // k_heads = 0: no keys
+  bool q_in_place, k_in_place;
+  int d;
+  int dims;         // of them turned
+  bool neighbours;  // pairs are dims 2 i and 2 i + 1, else i and i + dims / 2
+  bool inverse;
+  const double *freq;  // [dims / 2], radians per position
+  float amplitude;
+};
+int64_t kv_rotate_blocks(const KvRotate &R);
+km_status launch_kv_rotate(const KvRotate &R, int type, hipStream_t s);
 
 // kv_attend.hip
 struct KvAttend {
@@ -161,5 +207,21 @@ size_t kv_attend_scratch(const KvCache &C, const KvSeqs &S, const KvAttend &A);
 bool kv_attend_fits(const KvCache &C, const KvSeqs &S, const KvAttend &A);
 int64_t kv_attend_blocks(const KvCache &C, const KvSeqs &S, const KvAttend &A);
 km_status launch_kv_attend(const KvCache &C, const KvSeqs &S, const KvAttend &A, void *ws, hipStream_t s);
+
+
+// kv_weigh.hip: q, type, group, scale, causal, window and lse of A
+int64_t kv_weigh_blocks(const KvCache &C, const KvSeqs &S, const KvAttend &A);
+km_status launch_kv_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A, float *weight, float decay, hipStream_t s);
+
+// kv_evict.hip
+struct KvEvict {
+  float *weight;
+  const int32_t *keep;
+  int max_keep, first, recent;
+  int32_t *kept, *lens;
+};
+size_t kv_evict_scratch(const KvCache &C, const KvSeqs &S, int max_keep);
+int64_t kv_evict_blocks(const KvCache &C, const KvSeqs &S, int max_keep);
+km_status launch_kv_evict(const KvCache &C, const KvSeqs &S, const KvEvict &E, void *ws, hipStream_t s);
 
 }  // namespace kmq

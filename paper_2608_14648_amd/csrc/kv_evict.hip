@@ -1,0 +1,390 @@
+// Eviction: each sequence and head keeps its tokens of the largest weight and closes the gaps in its pages.
+//
+// Three kernels.  kv_select_kernel, a workgroup for each sequence and head: the K-th largest weight is found digit by digit (11, 11 and
+// 10 bits of the weights' ordered bit patterns, a histogram in LDS for each), then one pass in the order of positions writes down
+// who stays: all above it, and of those equal to it the first.  kv_gather_kernel, a workgroup for each page that tokens come to, keys or
+// values: builds the page's new contents in the workspace.  kv_scatter_kernel writes them over the page.  In place at once
+// a page could be written before another has taken its tokens from it: page t takes from pages t and later.  A page whose tokens
+// all stay where they are is left out of both.
+//
+// Bound by latency for one sequence (the passes over its weights, one workgroup to a head) and by HBM for many: codes are read and
+// written twice.
+#include "kv_pages.hpp"
+
+namespace kmq {
+namespace {
+
+constexpr int kSelect = 1024;  // threads
+constexpr int kOwn = 8;        // consecutive positions of a thread at a time
+constexpr int kBins = 2048;
+constexpr int kGather = 256;
+
+struct EvictArgs {
+  KvCache C;
+  KvSeqs S;
+  KvEvict E;
+  int tiles;        // pages that tokens may come to, of a sequence
+  int *moved;       // [n][heads][tiles]: the page's contents change
+  uint8_t *codes;   // [n][heads][tiles][2] pages of codes
+  float *scales;    // [n][heads][tiles][2]: of a page (8 bits) or of its tokens
+  float *weights;   // [n][heads][tiles][page]
+  uint32_t block0;
+};
+
+// False: the sequence is left as it is (its length does not fit, or one of its pages is not there).
+__device__ __forceinline__ bool evict_len(const KvCache &C, const KvSeqs &S, int b, int *len) {
+  *len = S.lens[b];
+  return *len >= 0 && (int64_t)*len <= (int64_t)S.max_pages * C.page;
+}
+
+// Ordered like the weights: NaN least, then -infinity to infinity.  Whole: counts as more than infinity.
+__device__ __forceinline__ uint32_t weight_key(float w, bool whole) {
+  const uint32_t u = __float_as_uint(w + 0.0f);  // -0 is 0
+  const uint32_t k = w == w ? u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u) : 0u;
+  return whole ? 0xffffffffu : k;
+}
+
+struct Count2 {
+  int more, same;
+};
+
+__global__ __launch_bounds__(kSelect) void kv_select_kernel(EvictArgs P) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ int wave_a[kSelect / 64], wave_b[kSelect / 64];
+  __shared__ uint32_t found[2];
+  const KvCache &C = P.C;
+  const KvEvict &E = P.E;
+  const int h = (int)(blockIdx.x % (uint32_t)C.heads), b = (int)(blockIdx.x / (uint32_t)C.heads);
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  int *kept = E.kept + ((int64_t)b * C.heads + h) * E.max_keep;
+  int *moved = P.moved + ((int64_t)b * C.heads + h) * P.tiles;
+  const int *table = P.S.table + (int64_t)b * P.S.table_ld;
+  int len;
+  bool fits = evict_len(C, P.S, b, &len);
+  if (fits) {
+    bool gone = false;
+    for (int p = t; p < (len + C.page - 1) >> C.shift; p += kSelect) gone = gone || table[p] < 0 || table[p] >= C.pages;
+    fits = !__syncthreads_or(gone);
+  }
+  const int K = fits ? min(len, max(0, min(E.keep[b], E.max_keep))) : 0;
+  if (h == 0 && t == 0) E.lens[b] = fits ? K : len;
+  for (int i = t; i < P.tiles; i += kSelect) moved[i] = 0;
+  for (int i = K + t; i < E.max_keep; i += kSelect) kept[i] = -1;
+  if (K == 0) return;
+  if (K == len) {
+    for (int i = t; i < K; i += kSelect) kept[i] = i;
+    return;
+  }
+  // a thread's next positions j .. j + 7 lie in one page
+  auto keys = [&](int j, uint32_t *k) {
+    const int pg = table[j >> C.shift];
+    const float *w = E.weight + ((int64_t)pg * C.heads + h) * C.page + (j & (C.page - 1));
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(w), z = *reinterpret_cast<const f32x4 *>(w + 4);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      k[i] = weight_key(i < 4 ? a[i] : z[i - 4], j + i < E.first || j + i >= len - E.recent);
+  };
+  uint32_t prefix = 0;
+  int left = K;  // how many to take of the keys that begin with prefix
+  constexpr int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = shifts[pass], bins = 1 << bits[pass];
+    for (int i = t; i < bins; i += kSelect) hist[i] = 0;
+    __syncthreads();
+    for (int j = kOwn * t; j < len; j += kOwn * kSelect) {
+      uint32_t k[kOwn];
+      keys(j, k);
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i)
+        if (j + i < len && (pass == 0 || k[i] >> (shift + bits[pass]) == prefix)) atomicAdd(&hist[(k[i] >> shift) & (bins - 1)], 1u);
+    }
+    __syncthreads();
+    // from the largest digit down: thread t has digits bins - 1 - each * t and the ones below it
+    const int each = bins / kSelect;  // 2 or 1
+    int mine = 0;
+    for (int i = 0; i < each; ++i) mine += (int)hist[bins - 1 - each * t - i];
+    int sum = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int y = __shfl_up(sum, o);
+      if (lane >= o) sum += y;
+    }
+    if (lane == 63) wave_a[wave] = sum;
+    __syncthreads();
+    int above = sum - mine;
+    for (int y = 0; y < wave; ++y) above += wave_a[y];
+    if (above < left && above + mine >= left) {
+      int i = 0;
+      for (; i < each - 1; ++i) {
+        const int n = (int)hist[bins - 1 - each * t - i];
+        if (above + n >= left) break;
+        above += n;
+      }
+      found[0] = (uint32_t)(bins - 1 - each * t - i);
+      found[1] = (uint32_t)(left - above);
+    }
+    __syncthreads();
+    prefix = (prefix << bits[pass]) | found[0];
+    left = (int)found[1];
+    __syncthreads();  // before hist, wave_a and found are written again
+  }
+  // those above the key `prefix`, and the first `left` of those equal to it, in the order of positions
+  int more0 = 0, same0 = 0;
+  for (int j0 = 0; j0 < len; j0 += kOwn * kSelect) {
+    const int j = j0 + kOwn * t;
+    uint32_t k[kOwn];
+    int more = 0, same = 0;
+    if (j < len) {
+      keys(j, k);
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        more += j + i < len && k[i] > prefix;
+        same += j + i < len && k[i] == prefix;
+      }
+    }
+    int ms = more, ss = same;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int y = __shfl_up(ms, o), z = __shfl_up(ss, o);
+      if (lane >= o) {
+        ms += y;
+        ss += z;
+      }
+    }
+    if (lane == 63) {
+      wave_a[wave] = ms;
+      wave_b[wave] = ss;
+    }
+    __syncthreads();
+    int mb = more0 + ms - more, sb = same0 + ss - same;
+    for (int y = 0; y < kSelect / 64; ++y) {
+      if (y < wave) {
+        mb += wave_a[y];
+        sb += wave_b[y];
+      }
+      more0 += wave_a[y];
+      same0 += wave_b[y];
+    }
+    if (j < len) {
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        if (j + i >= len) break;
+        const bool up = k[i] > prefix, eq = k[i] == prefix;
+        if (up || (eq && sb < left)) {
+          const int at = mb + min(sb, left);
+          kept[at] = j + i;
+          if (at != j + i) moved[at >> C.shift] = 1;
+        }
+        mb += up;
+        sb += eq;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+struct EvictTile {
+  int b, h, tile;
+  bool values;
+  int64_t bh, to;  // sequence and head; the page's head
+  int n;           // tokens that come to the page
+};
+__device__ __forceinline__ bool evict_tile(const EvictArgs &P, EvictTile *o) {
+  uint32_t x = P.block0 + blockIdx.x;
+  o->values = x & 1;
+  x >>= 1;
+  o->h = (int)(x % (uint32_t)P.C.heads);
+  x /= (uint32_t)P.C.heads;
+  o->tile = (int)(x % (uint32_t)P.tiles);
+  o->b = (int)(x / (uint32_t)P.tiles);
+  o->bh = (int64_t)o->b * P.C.heads + o->h;
+  if (!P.moved[o->bh * P.tiles + o->tile]) return false;  // then the sequence fits, and its pages are there
+  o->n = min(P.C.page, P.E.lens[o->b] - (o->tile << P.C.shift));
+  o->to = (int64_t)P.S.table[(int64_t)o->b * P.S.table_ld + o->tile] * P.C.heads + o->h;
+  return true;
+}
+
+template <int FMT>
+__global__ __launch_bounds__(kGather) void kv_gather_kernel(EvictArgs P) {
+  __shared__ int64_t from[128];  // page's head of each slot's token
+  __shared__ int tok[128];
+  __shared__ float was[128];
+  __shared__ float top[kGather / 64];
+  const KvCache &C = P.C;
+  EvictTile T;
+  if (!evict_tile(P, &T)) return;
+  const int t = threadIdx.x, page = C.page, d = C.d;
+  const int *kept = P.E.kept + T.bh * P.E.max_keep + ((int64_t)T.tile << C.shift);
+  const int *table = P.S.table + (int64_t)T.b * P.S.table_ld;
+  const float *scale = T.values ? C.vs : C.ks;
+  const int64_t slot = T.bh * P.tiles + T.tile;
+  float s = 0.0f;  // the largest scale of this wave's slots
+  if (t < page) {
+    // slots behind the last keep their own
+    const bool in = t < T.n;
+    const int pos = in ? kept[t] : 0;
+    const int64_t f = in ? (int64_t)table[pos >> C.shift] * C.heads + T.h : T.to;
+    const int k = in ? pos & (page - 1) : t;
+    from[t] = f;
+    tok[t] = k;
+    if constexpr (FMT == KM_KV_I4) {
+      P.scales[(2 * slot + T.values) * page + t] = scale[f * page + k];
+    } else {
+      s = scale[f];
+      was[t] = kv_mul_of_scale(s);
+      s = in ? s : 0.0f;
+    }
+    if (!T.values) P.weights[slot * page + t] = P.E.weight[f * page + k];
+  }
+  float mul = 0.0f;
+  bool again = false;
+  if constexpr (FMT != KM_KV_I4) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s = fmaxf(s, __shfl_xor(s, o));
+    if ((t & 63) == 0) top[t >> 6] = s;
+  }
+  __syncthreads();
+  if constexpr (FMT != KM_KV_I4) {
+    s = top[0];
+    for (int y = 1; y < kGather / 64; ++y) s = fmaxf(s, top[y]);
+    mul = kv_mul_of_scale(s);
+    if (t == 0) P.scales[2 * slot + T.values] = s;
+    if (t < T.n) again = was[t] > mul;
+    again = __syncthreads_or(again);
+  }
+  const int64_t hb = kv_bytes<FMT>((int64_t)page * d);
+  const int db = (int)kv_bytes<FMT>(d);
+  uint8_t *out = P.codes + (2 * slot + T.values) * hb;
+  // codes whose multiplier was larger, for the page's
+  auto coded = [&](uint32_t w, int i0, int di) {  // codes of slots i0, i0 + di, ...
+    if constexpr (FMT != KM_KV_I4) {
+      f16x2 lo, hi;
+      kv_widen4<FMT>(w, &lo, &hi);
+      float x[4] = {(float)lo.x, (float)lo.y, (float)hi.x, (float)hi.y};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) x[y] = x[y] * mul / fmaxf(was[i0 + y * di], mul);
+      const uint32_t z = code4<FMT, KM_T_BF16>(x, 1.0f);
+      uint32_t keep = 0;  // what lies behind the last slot
+#pragma unroll
+      for (int y = 0; y < 4; ++y) keep |= i0 + y * di < T.n && was[i0 + y * di] > mul ? 0u : 255u << (8 * y);
+      return (w & keep) | (z & ~keep);
+    }
+    return w;
+  };
+  if (!T.values) {
+    const int per = db / 16;
+    for (int i = t; i < page * per; i += kGather) {
+      const int r = i / per, c = i - r * per;
+      u32x4 w = *reinterpret_cast<const u32x4 *>(C.k + from[r] * hb + tok[r] * db + 16 * c);
+      if (again) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) w[y] = coded(w[y], r, 0);
+      }
+      *reinterpret_cast<u32x4 *>(out + r * db + 16 * c) = w;
+    }
+    return;
+  }
+  // 8 slots of a dim, neighbouring threads the slots of a dim's row
+  const int ng = page / 8;
+  for (int i = t; i < ng * d; i += kGather) {
+    const int c = i / ng, r0 = 8 * (i - c * ng);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const int r = r0 + y, k = tok[r];
+      if constexpr (FMT == KM_KV_I4) {
+        const uint32_t z = C.v[from[r] * hb + (c * page + k) / 2];
+        w[0] |= ((z >> (4 * (k & 1))) & 15u) << (4 * y);
+      } else {
+        w[y / 4] |= (uint32_t)C.v[from[r] * hb + c * page + k] << (8 * (y % 4));
+      }
+    }
+    if constexpr (FMT == KM_KV_I4) {
+      *reinterpret_cast<uint32_t *>(out + (c * page + r0) / 2) = w[0];
+    } else {
+      if (again) {
+        w[0] = coded(w[0], r0, 1);
+        w[1] = coded(w[1], r0 + 4, 1);
+      }
+      *reinterpret_cast<u32x2 *>(out + c * page + r0) = u32x2{w[0], w[1]};
+    }
+  }
+}
+
+template <int FMT>
+__global__ __launch_bounds__(kGather) void kv_scatter_kernel(EvictArgs P) {
+  const KvCache &C = P.C;
+  EvictTile T;
+  if (!evict_tile(P, &T)) return;
+  const int t = threadIdx.x, page = C.page;
+  const int64_t slot = T.bh * P.tiles + T.tile;
+  const int64_t hb = kv_bytes<FMT>((int64_t)page * C.d);
+  const u32x4 *in = reinterpret_cast<const u32x4 *>(P.codes + (2 * slot + T.values) * hb);
+  u32x4 *out = reinterpret_cast<u32x4 *>((T.values ? C.v : C.k) + T.to * hb);
+  for (int i = t; i < hb / 16; i += kGather) out[i] = in[i];
+  float *scale = T.values ? C.vs : C.ks;
+  if constexpr (FMT == KM_KV_I4) {
+    if (t < page) scale[T.to * page + t] = P.scales[(2 * slot + T.values) * page + t];
+  } else {
+    if (t == 0) scale[T.to] = P.scales[2 * slot + T.values];
+  }
+  if (!T.values && t < page) P.E.weight[T.to * page + t] = P.weights[slot * page + t];
+}
+
+int tiles_of(const KvCache &C, const KvSeqs &S, int max_keep) {
+  return (int)std::min<int64_t>(S.max_pages, cdiv(max_keep, C.page));
+}
+
+// Bytes of each part of the workspace, 16-byte aligned.
+struct Parts {
+  size_t moved, codes, scales, weights;
+};
+Parts parts_of(const KvCache &C, const KvSeqs &S, int max_keep) {
+  auto up = [](size_t x) { return (x + 15) & ~(size_t)15; };
+  const size_t slots = (size_t)S.n * C.heads * tiles_of(C, S, max_keep);
+  const bool i4 = C.fmt == KM_KV_I4;
+  return {up(4 * slots), up(2 * slots * C.page * C.d / (i4 ? 2 : 1)), up(8 * slots * (i4 ? C.page : 1)),
+          up(4 * slots * C.page)};
+}
+
+}  // namespace
+
+size_t kv_evict_scratch(const KvCache &C, const KvSeqs &S, int max_keep) {
+  const Parts p = parts_of(C, S, max_keep);
+  return p.moved + p.codes + p.scales + p.weights;
+}
+
+int64_t kv_evict_blocks(const KvCache &C, const KvSeqs &S, int max_keep) {
+  return (int64_t)2 * S.n * C.heads * tiles_of(C, S, max_keep);
+}
+
+km_status launch_kv_evict(const KvCache &C, const KvSeqs &S, const KvEvict &E, void *ws, hipStream_t s) {
+  const Parts p = parts_of(C, S, E.max_keep);
+  uint8_t *w = static_cast<uint8_t *>(ws);
+  EvictArgs P{C, S, E, tiles_of(C, S, E.max_keep), reinterpret_cast<int *>(w), w + p.moved,
+              reinterpret_cast<float *>(w + p.moved + p.codes), reinterpret_cast<float *>(w + p.moved + p.codes + p.scales), 0};
+  kv_select_kernel<<<dim3((unsigned)(S.n * C.heads)), kSelect, 0, s>>>(P);
+  KMQ_LAUNCH_CHECK("kv_evict");
+  const int64_t blocks = kv_evict_blocks(C, S, E.max_keep), most = kv_piece(kGather);
+  auto go = [&](auto *kernel) {
+    for (int64_t b = 0; b < blocks; b += most) {
+      P.block0 = (uint32_t)b;
+      kernel<<<dim3((unsigned)std::min(most, blocks - b)), kGather, 0, s>>>(P);
+    }
+  };
+  if (C.fmt == KM_KV_I8) {
+    go(kv_gather_kernel<KM_KV_I8>);
+    go(kv_scatter_kernel<KM_KV_I8>);
+  } else if (C.fmt == KM_KV_F8) {
+    go(kv_gather_kernel<KM_KV_F8>);
+    go(kv_scatter_kernel<KM_KV_F8>);
+  } else {
+    go(kv_gather_kernel<KM_KV_I4>);
+    go(kv_scatter_kernel<KM_KV_I4>);
+  }
+  KMQ_LAUNCH_CHECK("kv_evict");
+  return KM_OK;
+}
+
+}  // namespace kmq

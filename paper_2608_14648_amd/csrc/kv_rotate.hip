@@ -1,0 +1,217 @@
+// Rotary positions: queries and keys turned by the positions of their rows, before the cache takes them.
+//
+// Pair (x, y) of a head at position p, frequency f: (x cos pf - y sin pf, x sin pf + y cos pf), times an amplitude.  pf reaches 2^31
+// radians, so the turns pf / 2 pi and what is left of them past whole quarters are taken in 64 bits; the rest, at most pi / 4, goes
+// to fp32 and into the Taylor polynomials of sine and cosine (degree 9 and 10: below 2^-28 of 1 at pi / 4).  Products and their sums
+// are fp32, rounded once.
+//
+// Bound by HBM: each row is read and written once.  A workgroup takes some rows of a sequence, finds the sine and cosine of each
+// row's pairs once (all heads of a row share them, and 64-bit arithmetic for every head would cost more than the row's bytes) and
+// keeps them in LDS; a thread then turns VW pairs of a head at a time, in registers, so that rows may be turned in place.
+#include "kv.hpp"
+
+namespace kmq {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMostPairs = 512;  // sines and cosines of a workgroup's rows
+
+struct RotateArgs {
+  KvRotate R;
+  int tr;     // rows of a workgroup
+  int tiles;  // workgroups of a sequence
+  uint32_t block0;
+};
+
+// sine and cosine of `turns` turns
+__device__ __forceinline__ float2 turned(double turns) {
+  const double quarters = rint(4.0 * turns);
+  const float a = (float)((turns - 0.25 * quarters) * 6.283185307179586476925);
+  const int quad = (int)((long long)quarters & 3);
+  const float z = a * a;
+  float s = fmaf(z, 2.75573192e-6f, -1.98412698e-4f);  // 1 / 9!, 1 / 7!
+  s = fmaf(z, s, 8.33333333e-3f);
+  s = fmaf(z, s, -1.66666667e-1f);
+  s = fmaf(a * z, s, a);
+  float c = fmaf(z, -2.75573192e-7f, 2.48015873e-5f);  // 1 / 10!, 1 / 8!
+  c = fmaf(z, c, -1.38888889e-3f);
+  c = fmaf(z, c, 4.16666667e-2f);
+  c = fmaf(z, c, -0.5f);
+  c = fmaf(z, c, 1.0f);
+  const float sn = quad & 1 ? c : s, cn = quad & 1 ? s : c;
+  return float2{quad & 2 ? -sn : sn, (quad + 1) & 2 ? -cn : cn};
+}
+
+// N values of a row, from and to memory in pieces of at most 16 bytes
+template <int TYPE, int N>
+struct Vec {
+  static constexpr int bytes = N * KvElem<TYPE>::bytes;
+  static constexpr int words = bytes >= 4 ? bytes / 4 : 1;
+  uint32_t w[words];
+  __device__ __forceinline__ void load(const void *p, int64_t o) {
+    const char *a = static_cast<const char *>(p) + o * KvElem<TYPE>::bytes;
+    if constexpr (bytes >= 16) {
+#pragma unroll
+      for (int i = 0; i < words; i += 4) *reinterpret_cast<u32x4 *>(w + i) = *reinterpret_cast<const u32x4 *>(a + 4 * i);
+    } else if constexpr (bytes == 8) {
+      *reinterpret_cast<u32x2 *>(w) = *reinterpret_cast<const u32x2 *>(a);
+    } else if constexpr (bytes == 4) {
+      w[0] = *reinterpret_cast<const uint32_t *>(a);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t *>(a);
+    }
+  }
+  __device__ __forceinline__ void store(void *p, int64_t o) const {
+    char *a = static_cast<char *>(p) + o * KvElem<TYPE>::bytes;
+    if constexpr (bytes >= 16) {
+#pragma unroll
+      for (int i = 0; i < words; i += 4) *reinterpret_cast<u32x4 *>(a + 4 * i) = u32x4{w[i], w[i + 1], w[i + 2], w[i + 3]};
+    } else if constexpr (bytes == 8) {
+      *reinterpret_cast<u32x2 *>(a) = u32x2{w[0], w[1]};
+    } else if constexpr (bytes == 4) {
+      *reinterpret_cast<uint32_t *>(a) = w[0];
+    } else {
+      *reinterpret_cast<uint16_t *>(a) = (uint16_t)w[0];
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (TYPE == KM_T_F32) return __uint_as_float(w[i]);
+    const uint32_t h = w[i / 2] >> (16 * (i % 2));
+    if constexpr (TYPE == KM_T_BF16) return __uint_as_float(h << 16);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)h);
+  }
+  __device__ __forceinline__ void set(const float *x) {
+    if constexpr (TYPE == KM_T_F32) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = __float_as_uint(x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i += 2) w[i / 2] = kv_pack2<TYPE>(x[i], i + 1 < N ? x[i + 1] : 0.0f);
+    }
+  }
+};
+
+template <int TYPE, int VW>
+__global__ __launch_bounds__(kThreads) void kv_rotate_kernel(RotateArgs P) {
+  __shared__ float2 cs[kMostPairs];
+  const KvRotate &R = P.R;
+  const uint32_t x = P.block0 + blockIdx.x;
+  const int t = threadIdx.x, pairs = R.dims / 2;
+  int64_t row0, at;  // first row and its position
+  int nr;
+  if (R.positions) {
+    row0 = (int64_t)x * P.tr;
+    nr = (int)min((int64_t)P.tr, R.rows - row0);
+    at = 0;
+  } else {
+    const int b = (int)(x / (uint32_t)P.tiles), first = (int)(x - (uint32_t)b * P.tiles) * P.tr;
+    KvSeq q;
+    if (!kv_seq(R.S, 1 << 30, b, &q)) return;
+    nr = min(P.tr, q.n - first);
+    row0 = q.row0 + first;
+    at = (int64_t)q.len - q.n + first;
+  }
+  if (nr <= 0) return;
+  for (int i = t; i < nr * pairs; i += kThreads) {
+    const int r = i / pairs, p = i - r * pairs;
+    const int64_t pos = R.positions ? R.positions[row0 + r] : at + r;
+    float2 z = turned((double)pos * (R.freq[p] * 0.159154943091895335769));
+    cs[i] = float2{(R.inverse ? -z.x : z.x) * R.amplitude, z.y * R.amplitude};
+  }
+  __syncthreads();
+  const int units = R.d / (2 * VW), heads = R.q_heads + R.k_heads;  // a unit: VW pairs, or what is copied of as many
+  for (int i = t; i < nr * heads * units; i += kThreads) {
+    const int rh = i / units, c = i - rh * units;
+    const int r = rh / heads;
+    int h = rh - r * heads;
+    const bool key = h >= R.q_heads;
+    h -= key ? R.q_heads : 0;
+    const KvRows &in = key ? R.k : R.q, &out = key ? R.k_out : R.q_out;
+    const int64_t from = (row0 + r) * in.row + h * in.head, to = (row0 + r) * out.row + h * out.head;
+    const bool turn = c * VW < pairs;
+    if (!turn && (key ? R.k_in_place : R.q_in_place)) continue;
+    const int i0 = turn && !R.neighbours ? c * VW : 2 * c * VW;
+    const int i1 = turn && !R.neighbours ? i0 + pairs : i0 + VW;
+    Vec<TYPE, VW> a, b;
+    a.load(in.p, from + i0);
+    b.load(in.p, from + i1);
+    if (turn) {
+      const float2 *z = cs + r * pairs + c * VW;
+      float u[VW], v[VW];
+      if (!R.neighbours) {
+#pragma unroll
+        for (int y = 0; y < VW; ++y) {
+          const float p = a.get(y), q = b.get(y);
+          u[y] = fmaf(p, z[y].y, -(q * z[y].x));
+          v[y] = fmaf(p, z[y].x, q * z[y].y);
+        }
+      } else {
+        float w[2 * VW];
+#pragma unroll
+        for (int y = 0; y < VW; ++y) {
+          w[y] = a.get(y);
+          w[VW + y] = b.get(y);
+        }
+#pragma unroll
+        for (int y = 0; y < VW; ++y) {
+          const float p = w[2 * y], q = w[2 * y + 1];
+          w[2 * y] = fmaf(p, z[y].y, -(q * z[y].x));
+          w[2 * y + 1] = fmaf(p, z[y].x, q * z[y].y);
+        }
+#pragma unroll
+        for (int y = 0; y < VW; ++y) {
+          u[y] = w[y];
+          v[y] = w[VW + y];
+        }
+      }
+      a.set(u);
+      b.set(v);
+    }
+    a.store(out.p, to + i0);
+    b.store(out.p, to + i1);
+  }
+}
+
+// Rows of a workgroup: as many as fill its threads with pairs, one where the call then has fewer workgroups than there are CUs.
+int tile_rows(const KvRotate &R) {
+  const int64_t rows = R.positions ? R.rows : std::min<int64_t>(R.S.rows, (int64_t)R.S.n * R.S.max_rows);
+  const int most = std::max(1, std::min(8, kMostPairs / (R.dims / 2)));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, rows / 512));
+}
+
+}  // namespace
+
+int64_t kv_rotate_blocks(const KvRotate &R) {
+  const int tr = tile_rows(R);
+  return R.positions ? cdiv(R.rows, tr) : (int64_t)R.S.n * cdiv(R.S.max_rows, tr);
+}
+
+km_status launch_kv_rotate(const KvRotate &R, int type, hipStream_t s) {
+  RotateArgs P{R, tile_rows(R), 0, 0};
+  P.tiles = R.positions ? 1 : (int)cdiv(R.S.max_rows, P.tr);
+  const int64_t blocks = kv_rotate_blocks(R), most = kv_piece(kThreads);
+  const int pairs = R.dims / 2;
+  auto go = [&](auto *kernel) {
+    for (int64_t b = 0; b < blocks; b += most) {
+      P.block0 = (uint32_t)b;
+      kernel<<<dim3((unsigned)std::min(most, blocks - b)), kThreads, 0, s>>>(P);
+    }
+  };
+#define KV_V(T)                                    \
+  if (pairs % 8 == 0) go(kv_rotate_kernel<T, 8>);  \
+  else if (pairs % 4 == 0) go(kv_rotate_kernel<T, 4>); \
+  else if (pairs % 2 == 0) go(kv_rotate_kernel<T, 2>); \
+  else go(kv_rotate_kernel<T, 1>);
+  if (type == KM_T_F32) {
+    KV_V(KM_T_F32)
+  } else if (type == KM_T_BF16) {
+    KV_V(KM_T_BF16)
+  } else {
+    KV_V(KM_T_F16)
+  }
+#undef KV_V
+  KMQ_LAUNCH_CHECK("kv_rotate");
+  return KM_OK;
+}
+
+}  // namespace kmq
