@@ -413,7 +413,7 @@ typedef enum { KM_T_F32 = 0, KM_T_BF16 = 1, KM_T_F16 = 2 } km_type; /* rows give
  *   k: codes [pages][heads][page][d]; v: codes [pages][heads][d][page] (dims first: the attention sums over
  *   tokens).  k_scale, v_scale: float[pages][heads].  k and v 16-byte aligned.  A new cache needs no contents.
  *   I4: d % 32 == 0; k: bytes [pages][heads][page][d / 2]; v: bytes [pages][heads][d][page / 2]; k_scale, v_scale:
- *   float[pages][heads][page].
+ *   float[pages][heads][page], 16-byte aligned.
  */
 typedef struct km_kv_cache {
   int32_t fmt; /* km_kv_format */
@@ -551,10 +551,15 @@ km_status kv_rotate(const km_kv_rotary *rotary, const km_kv_seqs *seqs, const in
  *   weight: DEVICE float[pages][heads][page].  decay: finite, >= 0.  Sums are fp32, in an order that does not depend on scheduling.
  *   Positions on pages that are not there have no weight.  No two sequences of a call may have a page in common.
  *   q_heads, scale, flags, window, type: as in kv_attend; max_rows * q_heads / heads < 2^30.
+ *   ws (nullable): kv_weigh_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the pool.
  */
 km_status kv_weigh(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *q, int32_t q_heads, float scale,
-                   int32_t flags, int32_t window, int32_t type, const float *lse, float *weight, float decay,
-                   km_stream stream);
+                   int32_t flags, int32_t window, int32_t type, const float *lse, float *weight, float decay, void *ws,
+                   int64_t ws_bytes, km_stream stream);
+
+/* Bytes of ws that kv_weigh uses for these arguments (0: none; < 0: a km_status). */
+int64_t kv_weigh_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t q_heads, int32_t flags, int32_t window,
+                       int32_t type);
 
 /*
  * kv_evict -- every sequence keeps keep[b] of its tokens, each head its own, and closes the gaps: the first `first` and the last

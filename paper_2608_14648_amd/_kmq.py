@@ -25,7 +25,8 @@ STATUS = {0: "KM_OK", -1: "KM_EINVAL", -2: "KM_EUNSUPPORTED", -3: "KM_ENOMEM", -
 EXPORTS = ("quantize", "rabitq_encode", "pca_fit_cov", "pca_project", "kmeans_assign", "kmeans_assign_noalloc",
            "kmeans_update",
            "kmeans_fit", "kmeans_fine", "kmeans_fit_hier", "kmeans_assign_pruned", "kmeans_fit_pruned", "kmeans_cost",
-           "kv_write", "kv_read", "kv_attend", "kv_attend_bytes", "kv_rotate", "kv_weigh", "kv_evict", "kv_evict_bytes",
+           "kv_write", "kv_read", "kv_attend", "kv_attend_bytes", "kv_rotate", "kv_weigh", "kv_weigh_bytes", "kv_evict",
+           "kv_evict_bytes",
            "km_last_error", "km_release")
 
 
@@ -112,7 +113,8 @@ def lib():
             "kv_attend": [vp, vp, vp, i32, ct.c_float, i32, i32, vp, i32, vp, vp, i64, vp],
             "kv_attend_bytes": [vp, vp, i32, i32, i32, i32],
             "kv_rotate": [vp, vp, vp, i64, vp, i32, vp, i32, vp, vp, i32, i32, i32, vp],
-            "kv_weigh": [vp, vp, vp, i32, ct.c_float, i32, i32, i32, vp, vp, ct.c_float, vp],
+            "kv_weigh": [vp, vp, vp, i32, ct.c_float, i32, i32, i32, vp, vp, ct.c_float, vp, i64, vp],
+            "kv_weigh_bytes": [vp, vp, i32, i32, i32, i32],
             "kv_evict": [vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, i64, vp],
             "kv_evict_bytes": [vp, vp, i32],
             "km_release": [],
@@ -123,6 +125,7 @@ def lib():
             f.restype = ct.c_int
         L.kv_attend_bytes.restype = i64
         L.kv_evict_bytes.restype = i64
+        L.kv_weigh_bytes.restype = i64
         L.km_last_error.argtypes = []
         L.km_last_error.restype = ct.c_char_p
         _lib = L

@@ -377,10 +377,17 @@ def kv_weigh(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, lse: torch.Tensor, w
     if tuple(lse.shape) != (seqs.rows, q_heads):
         raise ValueError(f"lse must be [{seqs.rows}, {q_heads}] (got {tuple(lse.shape)})")
     _weights(weight, cache)
-    if seqs.rows:
-        _check(lib().kv_weigh(cache._ref, seqs._ref, ct.addressof(qr), q_heads,
-                              1.0 / math.sqrt(cache.d) if scale is None else scale, KM_KV_CAUSAL if causal else 0, _i32(window),
-                              _TYPES[q.dtype], lse.data_ptr(), weight.data_ptr(), decay, _raw_stream(cache.device.index)))
+    if seqs.rows == 0:
+        return
+    lb = lib()
+    flags, window, t = KM_KV_CAUSAL if causal else 0, _i32(window), _TYPES[q.dtype]
+    need = lb.kv_weigh_bytes(cache._ref, seqs._ref, q_heads, flags, window, t)
+    if need < 0:
+        raise KmqError(need, lb.km_last_error().decode(errors="replace"))
+    ws = torch.empty(need, dtype=torch.uint8, device=cache.device) if need else None
+    _check(lb.kv_weigh(cache._ref, seqs._ref, ct.addressof(qr), q_heads, 1.0 / math.sqrt(cache.d) if scale is None else scale,
+                       flags, window, t, lse.data_ptr(), weight.data_ptr(), decay, None if ws is None else ws.data_ptr(), need,
+                       _raw_stream(cache.device.index)))
 
 
 def kv_evict(cache: KvCache, seqs: KvSeqs, weight: torch.Tensor, keep: torch.Tensor, max_keep: int, first: int = 0,

@@ -1165,6 +1165,8 @@ static km_status check_cache(const km_kv_cache *c, KvCache *o) {
             (long long)c->pages);
   KMQ_CHECK(c->k && c->v && c->k_scale && c->v_scale, KM_EINVAL, "NULL argument");
   KMQ_CHECK(aligned16(c->k) && aligned16(c->v), KM_EINVAL, "codes must be 16-byte aligned");
+  KMQ_CHECK(c->fmt != KM_KV_I4 || (aligned16(c->k_scale) && aligned16(c->v_scale)), KM_EINVAL,
+            "scales of 4-bit codes must be 16-byte aligned");
   const int shift = c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
   *o = KvCache{c->fmt,   c->page, shift,      c->heads, c->d, c->pages, static_cast<uint8_t *>(c->k),
                static_cast<uint8_t *>(c->v), c->k_scale, c->v_scale};
@@ -1365,28 +1367,57 @@ km_status kv_rotate(const km_kv_rotary *rotary, const km_kv_seqs *seqs, const in
   return launch_kv_rotate(r, type, reinterpret_cast<hipStream_t>(stream));
 }
 
-km_status kv_weigh(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *q, int32_t q_heads, float scale,
-                   int32_t flags, int32_t window, int32_t type, const float *lse, float *weight, float decay,
-                   km_stream stream) {
+static km_status check_weigh(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t q_heads, int32_t flags, int32_t window,
+                             int32_t type, KvCache *c, KvSeqs *s, KvAttend *a) {
+  km_status st = check_cache(cache, c);
+  if (st == KM_OK) st = check_seqs(seqs, *c, s);
+  if (st == KM_OK) st = check_queries(*c, *s, q_heads, flags, window, type, a);
+  if (st != KM_OK) return st;
+  KMQ_CHECK(s->n < 2 || s->table_ld != 0, KM_EINVAL, "sequences of one table row share their pages' weights");
+  KMQ_CHECK((int64_t)s->n * c->heads <= (1 << 20), KM_EINVAL, "n * heads = %lld must be <= 2^20", (long long)s->n * c->heads);
+  return s->n ? check_grid(kv_weigh_blocks(*c, *s, *a)) : KM_OK;
+}
+
+int64_t kv_weigh_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t q_heads, int32_t flags, int32_t window,
+                       int32_t type) {
   g_err[0] = 0;
   KvCache c;
   KvSeqs s;
   KvAttend a;
-  km_status st = check_cache(cache, &c);
-  if (st == KM_OK) st = check_seqs(seqs, c, &s);
-  if (st == KM_OK) st = check_queries(c, s, q_heads, flags, window, type, &a);
+  const km_status st = check_weigh(cache, seqs, q_heads, flags, window, type, &c, &s, &a);
+  if (st != KM_OK) return st;
+  return s.n ? (int64_t)kv_weigh_scratch(c, s, a) : 0;
+}
+
+km_status kv_weigh(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *q, int32_t q_heads, float scale,
+                   int32_t flags, int32_t window, int32_t type, const float *lse, float *weight, float decay, void *ws,
+                   int64_t ws_bytes, km_stream stream) {
+  g_err[0] = 0;
+  KvCache c;
+  KvSeqs s;
+  KvAttend a;
+  km_status st = check_weigh(cache, seqs, q_heads, flags, window, type, &c, &s, &a);
   if (st != KM_OK) return st;
   KMQ_CHECK(scale > 0.0f && std::isfinite(scale), KM_EINVAL, "scale = %g must be finite and > 0", (double)scale);
   KMQ_CHECK(decay >= 0.0f && std::isfinite(decay), KM_EINVAL, "decay = %g must be finite and >= 0", (double)decay);
-  KMQ_CHECK(s.n < 2 || s.table_ld != 0, KM_EINVAL, "sequences of one table row share their pages' weights");
   if (s.n == 0) return KM_OK;
   KMQ_CHECK(lse != nullptr && weight != nullptr, KM_EINVAL, "NULL argument");
   st = check_rows(q, type, "q", &a.q);
-  if (st == KM_OK) st = check_grid(kv_weigh_blocks(c, s, a));
   if (st != KM_OK) return st;
   a.scale = scale;
   a.lse = const_cast<float *>(lse);  // read only
-  return launch_kv_weigh(c, s, a, weight, decay, reinterpret_cast<hipStream_t>(stream));
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const int64_t need = (int64_t)kv_weigh_scratch(c, s, a);
+  Scratch own(hs);
+  if (need && ws == nullptr) {
+    st = own.alloc((size_t)need);
+    if (st != KM_OK) return st;
+    ws = own.get();
+  } else if (need) {
+    KMQ_CHECK(ws_bytes >= need && aligned16(ws), KM_EINVAL, "ws needs %lld bytes (got %lld) and 16-byte alignment",
+              (long long)need, (long long)ws_bytes);
+  }
+  return launch_kv_weigh(c, s, a, weight, decay, ws, hs);
 }
 
 static km_status check_evict(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t max_keep, KvCache *c, KvSeqs *s) {

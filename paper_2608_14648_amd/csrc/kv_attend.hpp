@@ -82,8 +82,8 @@ __device__ __forceinline__ float far_add(float l, float x) { return fmaf(__built
 template <int FMT>
 using Codes16 = std::conditional_t<FMT == KM_KV_I4, u32x2, u32x4>;
 template <int FMT>
-__device__ __forceinline__ f16x8 widen8(const Codes16<FMT> &w, int k) {
-  if constexpr (FMT == KM_KV_I4) return kv_widen4x8(w[k]);
+__device__ __forceinline__ f16x8 widen8(const Codes16<FMT> &w, int k, const KvNibbles &nib) {
+  if constexpr (FMT == KM_KV_I4) return kv_widen4x8(w[k], nib);
   else return kv_widen8<FMT>(w[2 * k], w[2 * k + 1]);
 }
 template <int FMT>
@@ -297,6 +297,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
   const KvAttend &A = P.A;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   const int d = C.d, rows = q.n * A.group;
+  const KvNibbles nib = kv_nibbles();
 
   // Codes of a chunk.  Its page (ONE), or the pages of this lane's runs of 16: keys of run kr, values of run g.  Behind the
   // end and where a page is not there something of the cache is read that counts for nothing.
@@ -432,7 +433,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
       for (int p = 0; p < NP; ++p)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const f16x8 kf = widen8<FMT>(kw[st][p], k);
+          const f16x8 kf = widen8<FMT>(kw[st][p], k, nib);
 #pragma unroll
           for (int u = 0; u < RT; ++u)
 #pragma unroll
@@ -532,7 +533,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
       if (n % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const f16x8 vf = widen8<FMT>(vw[n], k);
+        const f16x8 vf = widen8<FMT>(vw[n], k, nib);
 #pragma unroll
         for (int u = 0; u < RT; ++u)
 #pragma unroll
@@ -605,8 +606,14 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &P, const KvSeq &q,
   }
 }
 
+// Waves to a SIMD that the registers have to leave room for.
+template <int FMT, int NT, int RT, int NS, int W>
+constexpr int attend_waves() {
+  return NT > 8 ? 1 : FMT == KM_KV_I4 && RT == 1 && NS == 1 && W == kAttendWaves ? 3 : 2;
+}
+
 template <int FMT, int NT, int RT, int NS, bool ONE, int W>
-__global__ __launch_bounds__(64 * W, NT <= 8 ? 2 : 1) void kv_attend_kernel(AttendArgs P) {
+__global__ __launch_bounds__(64 * W, (attend_waves<FMT, NT, RT, NS, W>())) void kv_attend_kernel(AttendArgs P) {
   __shared__ AttendWave<RT, NT> sh[W];
   constexpr int TR = 16 * RT;
   KvSeq q;
@@ -873,6 +880,7 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
   // accumulators then no longer fit beside the rest (256 dims: 760 us instead of 638).
   const int wave = ND <= 4 ? __builtin_amdgcn_readfirstlane(t >> 6) : t >> 6;
   const int d = C.d;
+  const KvNibbles nib = kv_nibbles();
   const int rw = r0 + 32 * wave;  // this wave's first row
 
   // the tiles of this wave's rows
@@ -951,7 +959,7 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
     if constexpr (I4) {
       f16x8 *o = reinterpret_cast<f16x8 *>(&kt[c & 1][p / PC * KLD + 32 * (p % PC)]);
 #pragma unroll
-      for (int y = 0; y < 4; ++y) o[y] = kv_widen4x8(from[i][y]);
+      for (int y = 0; y < 4; ++y) o[y] = kv_widen4x8(from[i][y], nib);
     } else {
       f16x8 *o = reinterpret_cast<f16x8 *>(&kt[c & 1][p / PC * KLD + 16 * (p % PC)]);
       o[0] = kv_widen8<FMT>(from[i].x, from[i].y);
@@ -966,8 +974,8 @@ __global__ __launch_bounds__(64 * kWaves, ND <= 4 ? 2 : 1) void kv_prompt_kernel
     if (VN % T != 0 && t + i * T >= VN) return;
     f16x8 *o = reinterpret_cast<f16x8 *>(&vt[c & 1][((t >> 2) + i * (T / 4)) * VLD + 16 * run]);
     if constexpr (I4) {
-      o[0] = kv_widen4x8(vc[i].x);
-      o[1] = kv_widen4x8(vc[i].y);
+      o[0] = kv_widen4x8(vc[i].x, nib);
+      o[1] = kv_widen4x8(vc[i].y, nib);
     } else {
       o[0] = kv_widen8<FMT>(vc[i].x, vc[i].y);
       o[1] = kv_widen8<FMT>(vc[i].z, vc[i].w);
@@ -1332,8 +1340,9 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
     // of 96 162 and 160; even splits are alike, but for one head, 100000 positions: 20 and 15.
     // Workgroups that run at a time with 128 dims, two waves to a SIMD (64 dims have room for three or four).
     const int64_t cap = (int64_t)S.max_pages * C.page / kChunk + 1 + kTileCost;  // whatever max_len says
-    const int64_t most = p.nt <= 8 ? 512 : 256;
-    const bool eight = p.nt <= 8 && A.type != KM_T_F32;
+    const bool three = C.fmt == KM_KV_I4 && p.nt <= 8 && p.rt == 1 && A.type != KM_T_F32;
+    const int64_t most = three ? 768 : p.nt <= 8 ? 512 : 256;
+    const bool eight = p.nt <= 8 && A.type != KM_T_F32 && !three;
     p.spread = p.tiles * p.rt < 256;
     const int64_t alone = p.tiles > 256    ? 32  // the most chunks of a tile that is not split up
                           : p.tiles >= 192 ? (eight ? 96 : 48)

@@ -18,7 +18,7 @@
 namespace kmq {
 namespace {
 
-constexpr int kWeighWaves = 4;
+constexpr int kFewWaves = 4, kManyWaves = 8;  // of a workgroup
 
 struct WeighArgs {
   KvCache C;
@@ -27,7 +27,8 @@ struct WeighArgs {
   float *weight;
   float decay;
   int groups;  // workgroups of a sequence's head
-  int many;    // waves share their positions
+  int step, step_tok, step_head;  // rows from a wave's tile to its next: tokens and heads of a token
+  uint32_t group_inverse;         // 2^32 / group, rounded up
   uint32_t block0;
 };
 
@@ -45,21 +46,23 @@ __device__ __forceinline__ float sum_row(float x) {
 }
 
 // TYPE: bf16 and fp16 rows as they are, fp32 rows in two halves (NS = 2)
-template <int FMT, int TYPE, int NP, bool ONE>
-__global__ __launch_bounds__(64 * kWeighWaves) void kv_weigh_kernel(WeighArgs P) {
-  constexpr int NS = TYPE == KM_T_F32 ? 2 : 1;
-  __shared__ float sh[kWeighWaves][kChunk];
+template <int FMT, int TYPE, int NP, bool MANY, bool ONE>
+__global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !MANY ? 3 : NP <= 3 ? 2 : 1)) void kv_weigh_kernel(
+    WeighArgs P) {
+  constexpr int NS = TYPE == KM_T_F32 ? 2 : 1, W = MANY ? kManyWaves : kFewWaves;
+  __shared__ float sh[MANY ? W : 1][kChunk];
   const KvCache &C = P.C;
   const KvAttend &A = P.A;
   uint32_t x = P.block0 + blockIdx.x;
   const int h = (int)(x % (uint32_t)C.heads);  // heads fastest: a head's workgroups share an XCD's L2 where they are a multiple of 8
   x /= (uint32_t)C.heads;
-  const int b = (int)(x / (uint32_t)P.groups);
+  // the sequences side by side: with many rows the first positions, which most rows see, begin first
+  const int b = (int)(x % (uint32_t)P.S.n), group = (int)(x / (uint32_t)P.S.n);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  const int group = (int)(x - (uint32_t)b * P.groups);
   KvSeq q;
   if (!kv_seq(P.S, C.page, b, &q) || q.n == 0) return;
   const int d = C.d, rows = q.n * A.group;
+  const KvNibbles nib = kv_nibbles();
   const int64_t hb = kv_bytes<FMT>((int64_t)C.page * d);
   const int db = (int)kv_bytes<FMT>(d);
   const int pmask = C.page - 1, last = q.len - 1, kr = m >> 2, ktok = m & 3;
@@ -70,9 +73,9 @@ __global__ __launch_bounds__(64 * kWeighWaves) void kv_weigh_kernel(WeighArgs P)
   };
   auto there_at = [&](int pg) { return pg >= 0 && pg < C.pages; };
   auto head_at = [&](int pg) { return (int64_t)(there_at(pg) ? pg : 0) * C.heads + h; };
-  // every wave's positions are behind the end at once (P.many), or no barrier follows
-  for (int64_t c = P.many ? group : (int64_t)group * kWeighWaves + wave; c * kChunk < q.len;
-       c += (int64_t)P.groups * (P.many ? 1 : kWeighWaves)) {
+  // every wave's positions are behind the end at once (MANY), or no barrier follows
+  for (int64_t c = MANY ? group : (int64_t)group * W + wave; c * kChunk < q.len;
+       c += (int64_t)P.groups * (MANY ? 1 : W)) {
   const int j0 = (int)c * kChunk;
   // positions of this lane's scores: run g; the keys that it loads: run kr
   const int pv = page_of(j0 + (ONE ? 0 : 16 * g)), pk = ONE ? pv : page_of(j0 + 16 * kr);
@@ -81,7 +84,7 @@ __global__ __launch_bounds__(64 * kWeighWaves) void kv_weigh_kernel(WeighArgs P)
   const int64_t at = head_at(pv) * C.page + (jm & pmask);
   const float old = mine && P.decay != 0.0f && jm < q.len - q.n ? P.weight[at] : 0.0f;
 
-  // keys, dims past d are 0 in the queries
+  // keys; dims past d are 0
   f16x8 kf[4][NP][2];
   {
     const uint8_t *kp = C.k + head_at(pk) * hb + ((j0 + (ONE ? 0 : 16 * kr)) & pmask) * db;
@@ -99,7 +102,8 @@ __global__ __launch_bounds__(64 * kWeighWaves) void kv_weigh_kernel(WeighArgs P)
       for (int p = 0; p < NP; ++p)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          kf[st][p][k] = widen8<FMT>(kw[st][p], k);
+          kf[st][p][k] = widen8<FMT>(kw[st][p], k, nib);
+          if (64 * p + 16 * g >= d) kf[st][p][k] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
           if constexpr (FMT == KM_KV_I4) {  // in the dims' order, as the queries lie
             const f16x8 y = kf[st][p][k];
             kf[st][p][k] = f16x8{y[0], y[2], y[4], y[6], y[1], y[3], y[5], y[7]};
@@ -130,44 +134,73 @@ __global__ __launch_bounds__(64 * kWeighWaves) void kv_weigh_kernel(WeighArgs P)
   int t0 = 0, t1 = q.n;
   if (A.causal) t0 = max(j0 - first, 0);
   if (A.window) t1 = (int)max((int64_t)0, min((int64_t)q.n, (int64_t)j0 + kChunk - 1 + A.window - first));
-  const int r1 = t1 * A.group;
-  int r0 = (int)min((int64_t)t0 * A.group, (int64_t)rows) + (P.many ? 16 * wave : 0);
-  const int step = P.many ? 16 * kWeighWaves : 16;
+  // From the last rows, which most positions are seen by, to the first: workgroups that begin together go through the same rows at
+  // the same time, and find them in L2.
+  const int r1 = t1 * A.group, r_lo = (int)min((int64_t)t0 * A.group, (int64_t)rows) & ~15;
+  int rt = ((r1 - 1) & ~15) - (MANY ? 16 * wave : 0);  // the first row of the tile that is loaded next
+  int tok = max(rt, 0) / A.group, hq = max(rt, 0) - tok * A.group;  // its token and its place among the token's heads
+  // Row rt + x (x < 16): tokens further on and place; a division by the group, as a product where that is exact.
+  auto row_of = [&](int x, int *dt, int *dh) {
+    const int y = hq + x;
+    *dt = A.group == 1 ? y : A.group >= 16 ? (y >= A.group) : (int)__umulhi((uint32_t)y, P.group_inverse);
+    *dh = y - *dt * A.group;
+  };
+  auto offset_of = [&](int dt, int dh) { return (int64_t)dt * A.q.row + (int64_t)dh * A.q.head; };
+  u32x4 raw[NP][2 * NS];
+  float lse;
+  int pos;  // of this lane's row
+  auto load = [&] {
+    const char *base = static_cast<const char *>(A.q.p) +
+                       ((q.row0 + tok) * A.q.row + (int64_t)h * A.group * A.q.head) * (2 * NS);  // of the tile's token
+    int dt, dh;
+    row_of(m, &dt, &dh);
+    const bool in = rt + m < r1;  // rows behind the last: the tile's token's first one, which does not count there
+    pos = first + min(tok + dt, q.n - 1);
+    lse = in ? A.lse[(q.row0 + tok + dt) * C.heads * A.group + h * A.group + dh] : INFINITY;
+    const char *qp = base + (in ? offset_of(dt, dh) * (2 * NS) : 0);
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int i = 0; i < 2 * NS; ++i)
+        raw[p][i] = reinterpret_cast<const u32x4 *>(qp + 2 * NS * min(64 * p + 16 * g, d - 16))[i];
+  };
+  auto next = [&] {
+    rt -= P.step;
+    tok -= P.step_tok;
+    hq -= P.step_head;
+    if (hq < 0) {
+      hq += A.group;
+      --tok;
+    }
+  };
 
   float sum[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) sum[e] = 0.0f;
-  for (; r0 < r1; r0 += step) {
-    const int r = min(r0 + m, rows - 1);
-    const RowAt row = row_at(A, C, q, h, r);
-    const float lse = r0 + m < r1 ? A.lse[row.lse] : INFINITY;
+  if (rt >= r_lo) load();
+  while (rt >= r_lo) {
     const bool counts = fabsf(lse) < INFINITY;
     const float nl = counts ? -lse * kLog2e : -INFINITY;
-    const char *qp = static_cast<const char *>(A.q.p) + row.q * (2 * NS);
     f16x8 qf[NP][2][NS];
     float c32 = 1.0f;
+    if (!__all(counts)) {  // rows that do not count may hold NaN
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int k = 0; k < 2 * NS; ++k) raw[p][k] = counts ? raw[p][k] : u32x4{0, 0, 0, 0};
+    }
     if constexpr (NS == 1) {
 #pragma unroll
       for (int p = 0; p < NP; ++p)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          u32x4 w = *reinterpret_cast<const u32x4 *>(qp + 2 * (min(64 * p + 16 * g, d - 16) + 8 * k));
-          if (!counts || 64 * p + 16 * g >= d) w = u32x4{0, 0, 0, 0};  // rows that do not count may hold NaN
-          qf[p][k][0] = __builtin_bit_cast(f16x8, w);
-        }
+        for (int k = 0; k < 2; ++k) qf[p][k][0] = __builtin_bit_cast(f16x8, raw[p][k]);
     } else {
       float v[NP][16], top = 0.0f;
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        u32x4 raw[4];
+        values16<2>(raw[p], KM_T_F32, v[p]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = reinterpret_cast<const u32x4 *>(qp + 4 * min(64 * p + 16 * g, d - 16))[i];
-        values16<2>(raw, KM_T_F32, v[p]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if (!counts || 64 * p + 16 * g >= d) v[p][i] = 0.0f;
-          top = fmaxf(top, fabsf(v[p][i]));
-        }
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(v[p][i]));
       }
       float f;
       q_scale(max_groups(top), 1.0f / kLog2e, &f, &c32);
@@ -181,34 +214,38 @@ __global__ __launch_bounds__(64 * kWeighWaves) void kv_weigh_kernel(WeighArgs P)
           qf[p][i / 8][1][i % 8] = (_Float16)(y - (float)y16);
         }
     }
+    // positions that the row sees; the next rows are on their way meanwhile
+    const int see0 = A.window ? max(pos + 1 - A.window, 0) : 0, see1 = A.causal ? max(pos + 1, 0) : q.len;
+    next();
+    if (rt >= r_lo) load();
     f32x4 s[4];
 #pragma unroll
-    for (int st = 0; st < 4; ++st) {
-      s[st] = f32x4{0, 0, 0, 0};
+    for (int st = 0; st < 4; ++st) s[st] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int p = 0; p < NP; ++p)
+    for (int p = 0; p < NP; ++p)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-          for (int z = 0; z < NS; ++z) {
+        for (int z = 0; z < NS; ++z)
+#pragma unroll
+          for (int st = 0; st < 4; ++st) {  // four sums in turn: none waits for its last product
             if constexpr (TYPE == KM_T_BF16)
               s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[st][p][k]),
                                                               __builtin_bit_cast(bf16x8, qf[p][k][z]), s[st], 0, 0, 0);
             else
               s[st] = mfma16(kf[st][p][k], qf[p][k][z], s[st]);
           }
-    }
     if constexpr (NS == 2) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e / 4][e % 4] *= c32;
     }
-    int lo, hi;
-    row_span(A, q, r, &lo, &hi);
-    if (!__all(j0 >= lo && j0 + kChunk <= hi)) {
+    if (!__all(j0 >= see0 && j0 + kChunk <= see1)) {
+      int jg = j0 + 16 * g;
+      asm volatile("" : "+v"(jg));  // a branch: few tiles need it, so nothing of it is kept in registers
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int j = j0 + 16 * g + e;
-        if (j < lo || j >= hi) s[e / 4][e % 4] = -INFINITY;
+        const int j = jg + e;
+        if (j < see0 || j >= see1) s[e / 4][e % 4] = -INFINITY;
       }
     }
 #pragma unroll
@@ -221,70 +258,346 @@ __global__ __launch_bounds__(64 * kWeighWaves) void kv_weigh_kernel(WeighArgs P)
     const float z = sum_row(sum[e]);
     total = m == e ? z : total;
   }
-  if (P.many) {
+  if (MANY) {
     sh[wave][16 * g + m] = total;
     __syncthreads();
     total = 0.0f;
 #pragma unroll
-    for (int y = 0; y < kWeighWaves; ++y) total += sh[y][16 * g + m];
+    for (int y = 0; y < W; ++y) total += sh[y][16 * g + m];
     __syncthreads();  // before the next positions' sums
   }
-  if (mine && (!P.many || wave == 0)) P.weight[at] = fmaf(old, P.decay, total);
+  if (mine && (!MANY || wave == 0)) P.weight[at] = fmaf(old, P.decay, total);
   }
 }
 
 
-// One wave per 64 positions and rows in turn, or all rows to each wave.
-bool many_rows(const KvSeqs &S, const KvAttend &A) { return (int64_t)S.max_rows * A.group > 64; }
+// ---- many 16-bit rows ---------------------------------------------------------------------------------------------------
+//
+// A workgroup takes 256 positions, 64 to a wave, which stay in registers as the first operand of the 32 x 32 x 16 products, and
+// the waves share tiles of 32 tokens of one query head, which pass through LDS (two buffers, a tile's loads a tile ahead).  The
+// tiles of the rows that see the positions are split evenly over `splits` workgroups, whose sums kv_weigh_join_kernel adds up in order.
+constexpr int kRowWaves = 4, kRowKeys = kRowWaves * kChunk, kRowTile = 32;
 
-// Workgroups of a sequence's head: one for each of its pieces by the longest length that the caller knows, fewer where that is
-// more than 2^20 in all (a workgroup then takes several, as where a length is longer than was said).
-int groups_of(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
-  const int64_t pieces = cdiv(S.max_len, many_rows(S, A) ? kChunk : kChunk * kWeighWaves);
-  return (int)std::max<int64_t>(1, std::min(pieces, (1 << 20) / ((int64_t)S.n * C.heads)));
+struct WeighRows {
+  WeighArgs W;
+  int splits;
+  float *part;  // [n][heads][splits][groups * kRowKeys]
+};
+
+__device__ __forceinline__ bool weigh_split(const WeighRows &R, const KvSeq &q) {  // a longer one than was said is not split
+  return R.splits > 1 && q.len <= R.W.groups * kRowKeys;
+}
+
+template <int FMT, int TYPE, int ND, bool ONE>
+__global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows_kernel(WeighRows R) {
+  constexpr int T = 64 * kRowWaves, KS = 2 * ND, LD = 64 * ND + 16;  // bytes of a row in LDS, so that rows lie in different banks
+  constexpr int NI = (ND + 1) / 2;                                   // 16-byte pieces of a tile to a thread
+  __shared__ __align__(16) uint8_t qt[2][kRowTile * LD];
+  __shared__ float stat[2][kRowTile];
+  const WeighArgs &P = R.W;
+  const KvCache &C = P.C;
+  const KvAttend &A = P.A;
+  uint32_t x = P.block0 + blockIdx.x;
+  const int h = (int)(x % (uint32_t)C.heads);  // heads fastest: a head's workgroups share an XCD's L2 where they are a multiple of 8
+  x /= (uint32_t)C.heads;
+  const int b = (int)(x % (uint32_t)P.S.n);
+  x /= (uint32_t)P.S.n;
+  // the first positions, which most rows see, begin first
+  const int split = (int)(x % (uint32_t)R.splits), group0 = (int)(x / (uint32_t)R.splits);
+  KvSeq q;
+  if (!kv_seq(P.S, C.page, b, &q) || q.n == 0) return;
+  const bool parts = weigh_split(R, q);
+  if (!parts && split > 0) return;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), m = lane & 31, g = lane >> 5;
+  const int d = C.d, first = q.len - q.n;  // position of token 0
+  const int64_t hb = kv_bytes<FMT>((int64_t)C.page * d);
+  const int db = (int)kv_bytes<FMT>(d), pmask = C.page - 1, last = q.len - 1;
+  const int *table = P.S.table + (int64_t)b * P.S.table_ld;
+  auto page_of = [&](int j) {
+    const int pg = table[min(j, last) >> C.shift];
+    return ONE ? __builtin_amdgcn_readfirstlane(pg) : pg;
+  };
+  auto there_at = [&](int pg) { return pg >= 0 && pg < C.pages; };
+  auto head_at = [&](int pg) { return (int64_t)(there_at(pg) ? pg : 0) * C.heads + h; };
+  const KvNibbles nib = kv_nibbles();
+  const int per = d / 8;  // pieces of a row
+  int prow[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) prow[i] = (t + i * T) / per;
+
+  for (int64_t gi = group0; gi * kRowKeys < q.len; gi += P.groups) {
+    const int w0 = (int)gi * kRowKeys, j0 = w0 + wave * kChunk;
+    const bool mine = j0 < q.len;
+    // keys: row m of operand tt is position 32 tt + m
+    f16x8 kf[2][KS];
+    float ck[FMT == KM_KV_I4 ? 32 : 4];  // what a score is multiplied by; not 0, so that -infinity stays
+    if (mine) {
+      const float f = A.scale * kLog2e;
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        const int j = j0 + 32 * tt + m, pg = page_of(ONE ? j0 : j);
+        const uint8_t *kp = C.k + head_at(pg) * hb + (j & pmask) * db;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const uint8_t *from = kp + (int)kv_bytes<FMT>(min(16 * k + 8 * g, d - 8));
+          f16x8 y;
+          if constexpr (FMT == KM_KV_I4) {
+            y = kv_widen4x8(*reinterpret_cast<const uint32_t *>(from), nib);
+            y = f16x8{y[0], y[2], y[4], y[6], y[1], y[3], y[5], y[7]};  // in the dims' order, as the queries lie
+          } else {
+            const u32x2 w = *reinterpret_cast<const u32x2 *>(from);
+            y = kv_widen8<FMT>(w.x, w.y);
+          }
+          if (16 * k + 8 * g >= d) y = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+          if constexpr (TYPE == KM_T_BF16) {
+            typedef float f32x8 __attribute__((ext_vector_type(8)));
+            y = __builtin_bit_cast(f16x8, __builtin_convertvector(__builtin_convertvector(y, f32x8), bf16x8));
+          }
+          kf[tt][k] = y;
+        }
+      }
+      if constexpr (FMT == KM_KV_I4) {
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {  // positions 8 y + 4 g of the 64 and the next three: elements 4 y on
+          const int j = j0 + 8 * y + 4 * g, pg = page_of(ONE ? j0 : j);
+          const f32x4 ks = *reinterpret_cast<const f32x4 *>(C.ks + head_at(pg) * C.page + (j & pmask));
+#pragma unroll
+          for (int z = 0; z < 4; ++z) ck[4 * y + z] = there_at(pg) && j + z < q.len ? fmaxf(f * ks[z], 0x1p-126f) : 1.0f;
+        }
+      } else {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {  // runs of 16
+          const int j = j0 + 16 * y, pg = page_of(ONE ? j0 : j);
+          ck[y] = there_at(pg) && j < q.len ? fmaxf(f * C.ks[head_at(pg)], 0x1p-126f) : 1.0f;
+        }
+      }
+    }
+    // tiles of the tokens that see one of the positions: blocks [b0, b1) of 32 tokens, of one query head after the other
+    int t0 = 0, t1 = q.n;
+    if (A.causal) t0 = max(w0 - first, 0);
+    if (A.window) t1 = (int)max((int64_t)0, min((int64_t)q.n, (int64_t)w0 + kRowKeys - 1 + A.window - first));
+    const int b0 = t0 / kRowTile, b1 = max((t1 + kRowTile - 1) / kRowTile, b0), nb = b1 - b0;
+    const int64_t tiles = (int64_t)nb * A.group, ns = parts ? R.splits : 1;
+    const int z0 = (int)(tiles * split / ns), z1 = (int)(tiles * (split + 1) / ns);
+    int lh = nb ? z0 / nb : 0, lb = b0 + z0 - lh * nb;  // head and block of the tile that is loaded next
+    u32x4 raw[NI];
+    float lse[NI];
+    auto load = [&] {
+      const int64_t row = q.row0 + (int64_t)lb * kRowTile;
+      const uint16_t *base = static_cast<const uint16_t *>(A.q.p) + row * A.q.row + (int64_t)(h * A.group + lh) * A.q.head;
+      const int left = q.n - lb * kRowTile;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const bool in = prow[i] < min(left, kRowTile);
+        const int r = in ? prow[i] : 0, c = in ? t + i * T - r * per : 0;
+        raw[i] = *reinterpret_cast<const u32x4 *>(base + r * A.q.row + 8 * c);
+        lse[i] = in ? A.lse[(row + r) * C.heads * A.group + h * A.group + lh] : INFINITY;
+      }
+      if (++lb == b1) {
+        lb = b0;
+        ++lh;
+      }
+    };
+    auto store = [&](int z) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        if (prow[i] >= kRowTile) continue;
+        const bool counts = fabsf(lse[i]) < INFINITY;  // rows that do not count may hold NaN
+        const int c = t + i * T - prow[i] * per;
+        *reinterpret_cast<u32x4 *>(&qt[z & 1][prow[i] * LD + 16 * c]) = counts ? raw[i] : u32x4{0, 0, 0, 0};
+        if (c == 0) stat[z & 1][prow[i]] = counts ? -lse[i] * kLog2e : -INFINITY;
+      }
+    };
+    float sum[32];
+#pragma unroll
+    for (int e = 0; e < 32; ++e) sum[e] = 0.0f;
+    int cb = lb;  // block of the tile at hand
+    if (z0 < z1) {
+      load();
+      store(z0);
+      if (z0 + 1 < z1) load();
+      __syncthreads();
+    }
+    for (int z = z0; z < z1; ++z) {
+      if (z + 1 < z1) store(z + 1);
+      if (z + 2 < z1) load();
+      const int pos0 = first + cb * kRowTile;  // position of the tile's first token
+      if (mine && (!A.causal || pos0 + kRowTile > j0) && (!A.window || (int64_t)pos0 < (int64_t)j0 + kChunk - 1 + A.window)) {
+        f32x16v s[2];
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[tt][i] = 0.0f;
+        const uint8_t *from = &qt[z & 1][m * LD];
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const f16x8 y = *reinterpret_cast<const f16x8 *>(from + 2 * min(16 * k + 8 * g, d - 8));
+#pragma unroll
+          for (int tt = 0; tt < 2; ++tt) {
+            if constexpr (TYPE == KM_T_BF16)
+              s[tt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[tt][k]), __builtin_bit_cast(bf16x8, y),
+                                                              s[tt], 0, 0, 0);
+            else
+              s[tt] = mfma32(kf[tt][k], y, s[tt]);
+          }
+        }
+        const float nl = stat[z & 1][m];
+        const int pos = pos0 + m;
+        const int see0 = A.window ? max(pos + 1 - A.window, 0) : 0, see1 = A.causal ? max(pos + 1, 0) : q.len;
+        if (!__all(j0 >= see0 && j0 + kChunk <= see1)) {
+          int jg = j0 + 4 * g;
+          asm volatile("" : "+v"(jg));  // a branch: few tiles need it, so nothing of it is kept in registers
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const int j = jg + 8 * (e >> 2) + (e & 3);
+            if (j < see0 || j >= see1 || j >= q.len) s[e >> 4][e & 15] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          sum[e] += __builtin_amdgcn_exp2f(fmaf(s[e >> 4][e & 15], ck[FMT == KM_KV_I4 ? e : e >> 3], nl));
+      }
+      if (++cb == b1) cb = b0;
+      __syncthreads();
+    }
+    if (!mine) continue;
+    // over the 32 tokens; lane m of a half then holds element m of its 32
+    float total = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      float y = sum_row(sum[e]);
+      y += __shfl_xor(y, 16);
+      total = m == e ? y : total;
+    }
+    const int j = j0 + 8 * (m >> 2) + 4 * g + (m & 3), pg = page_of(ONE ? j0 : j);
+    if (j >= q.len || !there_at(pg)) continue;
+    if (parts) {
+      R.part[(((int64_t)b * C.heads + h) * R.splits + split) * P.groups * kRowKeys + j] = total;
+    } else {
+      float *w = P.weight + head_at(pg) * C.page + (j & pmask);
+      *w = fmaf(P.decay != 0.0f && j < first ? *w : 0.0f, P.decay, total);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void kv_weigh_join_kernel(WeighRows R) {
+  const WeighArgs &P = R.W;
+  const KvCache &C = P.C;
+  uint32_t x = P.block0 + blockIdx.x;
+  const int gi = (int)(x % (uint32_t)P.groups);
+  x /= (uint32_t)P.groups;
+  const int h = (int)(x % (uint32_t)C.heads), b = (int)(x / (uint32_t)C.heads);
+  KvSeq q;
+  if (!kv_seq(P.S, C.page, b, &q) || q.n == 0 || !weigh_split(R, q)) return;
+  const int j = gi * kRowKeys + threadIdx.x;
+  if (j >= q.len) return;
+  const int64_t pg = P.S.table[(int64_t)b * P.S.table_ld + (j >> C.shift)];
+  if (pg < 0 || pg >= C.pages) return;
+  const float *p = R.part + ((int64_t)b * C.heads + h) * R.splits * P.groups * kRowKeys + j;
+  float total = 0.0f;
+  for (int y = 0; y < R.splits; ++y) total += p[(int64_t)y * P.groups * kRowKeys];
+  float *w = P.weight + (pg * C.heads + h) * C.page + (j & (C.page - 1));
+  *w = fmaf(P.decay != 0.0f && j < q.len - q.n ? *w : 0.0f, P.decay, total);
+}
+
+// How a call is cut up.
+enum WeighWay {
+  kFew,    // each wave its own positions, all rows in turn
+  kShare,  // fp32 rows: a workgroup's waves share 64 positions and take the rows in turn
+  kRows    // 16-bit rows: kv_weigh_rows_kernel
+};
+struct WeighPlan {
+  WeighWay way;
+  int groups, splits;
+};
+WeighPlan plan_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
+  WeighPlan p{kFew, 1, 1};
+  const int64_t heads = (int64_t)S.n * C.heads, rows = (int64_t)S.max_rows * A.group;
+  if (A.type == KM_T_F32 ? rows > 64 : S.max_rows >= kRowTile) p.way = A.type == KM_T_F32 ? kShare : kRows;
+  // Workgroups of a sequence's head: one for each of its pieces by the longest length that the caller knows, fewer where that is
+  // more than 2^20 in all (a workgroup then takes several, as where a length is longer than was said).
+  const int64_t pieces = cdiv(S.max_len, p.way == kShare ? kChunk : p.way == kRows ? kRowKeys : kChunk * kFewWaves);
+  p.groups = (int)std::max<int64_t>(1, std::min(pieces, (1 << 20) / heads));
+  // three times as many workgroups as run at a time, of eight tiles at least
+  if (p.way == kRows)
+    p.splits = (int)std::max<int64_t>(1, std::min(cdiv(1536, heads * p.groups), cdiv(S.max_rows, kRowTile) * A.group / 8));
+  return p;
 }
 
 }  // namespace
 
 int64_t kv_weigh_blocks(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
-  return (int64_t)S.n * C.heads * groups_of(C, S, A);
+  const WeighPlan p = plan_weigh(C, S, A);
+  return (int64_t)S.n * C.heads * p.groups * p.splits;
 }
 
-km_status launch_kv_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A, float *weight, float decay, hipStream_t s) {
-  WeighArgs P{C, S, A, weight, decay, groups_of(C, S, A), many_rows(S, A), 0};
-  const int64_t blocks = kv_weigh_blocks(C, S, A), most = kv_piece(64 * kWeighWaves);
-  auto go = [&](auto *kernel) {
+size_t kv_weigh_scratch(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
+  const WeighPlan p = plan_weigh(C, S, A);
+  return p.splits > 1 ? sizeof(float) * (size_t)S.n * C.heads * p.splits * p.groups * kRowKeys : 0;
+}
+
+km_status launch_kv_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A, float *weight, float decay, void *ws,
+                          hipStream_t s) {
+  const WeighPlan p = plan_weigh(C, S, A);
+  const int waves = p.way == kShare ? kManyWaves : p.way == kRows ? kRowWaves : kFewWaves, threads = 64 * waves;
+  const int step = p.way == kShare ? 16 * waves : 16;
+  WeighRows R{{C, S, A, weight, decay, p.groups, step, step / A.group, step % A.group,
+               (uint32_t)((((uint64_t)1 << 32) + A.group - 1) / A.group), 0},
+              p.splits, static_cast<float *>(ws)};
+  auto go = [&](auto *kernel, const auto &args, int64_t blocks) {
+    const int64_t most = kv_piece(threads);
+    auto a = args;
     for (int64_t b = 0; b < blocks; b += most) {
-      P.block0 = (uint32_t)b;
-      kernel<<<dim3((unsigned)std::min(most, blocks - b)), 64 * kWeighWaves, 0, s>>>(P);
+      if constexpr (std::is_same_v<decltype(a), WeighRows>) a.W.block0 = (uint32_t)b;
+      else a.block0 = (uint32_t)b;
+      kernel<<<dim3((unsigned)std::min(most, blocks - b)), threads, 0, s>>>(a);
     }
   };
-#define KV_P(F, T, N) \
-  case N: \
-    C.page >= kChunk ? go(kv_weigh_kernel<F, T, N, true>) : go(kv_weigh_kernel<F, T, N, false>); \
-    break;
-#define KV_T(F, T)                 \
-  switch ((int)cdiv(C.d, 64)) {    \
-    KV_P(F, T, 1)                  \
-    KV_P(F, T, 2)                  \
-    KV_P(F, T, 3)                  \
-    KV_P(F, T, 4)                  \
+  const int64_t blocks = kv_weigh_blocks(C, S, A);
+#define KV_ONE(K, ...) C.page >= kChunk ? go(K<__VA_ARGS__, true>, KV_ARGS, blocks) : go(K<__VA_ARGS__, false>, KV_ARGS, blocks)
+#define KV_ARGS R.W
+#define KV_P(F, T, M)                                            \
+  switch ((int)cdiv(C.d, 64)) {                                  \
+    case 1: KV_ONE(kv_weigh_kernel, F, T, 1, M); break;          \
+    case 2: KV_ONE(kv_weigh_kernel, F, T, 2, M); break;          \
+    case 3: KV_ONE(kv_weigh_kernel, F, T, 3, M); break;          \
+    default: KV_ONE(kv_weigh_kernel, F, T, 4, M);                \
   }
-#define KV_F(F)                              \
-  if (A.type == KM_T_F32) KV_T(F, KM_T_F32)  \
-  else if (A.type == KM_T_BF16) KV_T(F, KM_T_BF16) \
-  else KV_T(F, KM_T_F16)
-  if (C.fmt == KM_KV_I8) {
-    KV_F(KM_KV_I8)
-  } else if (C.fmt == KM_KV_F8) {
-    KV_F(KM_KV_F8)
-  } else {
-    KV_F(KM_KV_I4)
+#define KV_R(F, T)                                               \
+  switch (dim_tiles32(C.d)) {                                    \
+    case 2: KV_ONE(kv_weigh_rows_kernel, F, T, 2); break;        \
+    case 3: KV_ONE(kv_weigh_rows_kernel, F, T, 3); break;        \
+    case 4: KV_ONE(kv_weigh_rows_kernel, F, T, 4); break;        \
+    case 6: KV_ONE(kv_weigh_rows_kernel, F, T, 6); break;        \
+    default: KV_ONE(kv_weigh_rows_kernel, F, T, 8);              \
   }
-#undef KV_F
-#undef KV_T
+  auto of_format = [&](auto fmt) {
+    constexpr int F = decltype(fmt)::value;
+    if (p.way == kShare) {
+      KV_P(F, KM_T_F32, true)
+    } else if (p.way == kFew) {
+      if (A.type == KM_T_F32) KV_P(F, KM_T_F32, false)
+      else if (A.type == KM_T_BF16) KV_P(F, KM_T_BF16, false)
+      else KV_P(F, KM_T_F16, false)
+    } else {
+#undef KV_ARGS
+#define KV_ARGS R
+      if (A.type == KM_T_BF16) KV_R(F, KM_T_BF16)
+      else KV_R(F, KM_T_F16)
+    }
+  };
+  if (C.fmt == KM_KV_I8) of_format(std::integral_constant<int, KM_KV_I8>{});
+  else if (C.fmt == KM_KV_F8) of_format(std::integral_constant<int, KM_KV_F8>{});
+  else of_format(std::integral_constant<int, KM_KV_I4>{});
+#undef KV_R
 #undef KV_P
+#undef KV_ARGS
+#undef KV_ONE
   KMQ_LAUNCH_CHECK("kv_weigh");
+  if (p.splits > 1) {
+    go(kv_weigh_join_kernel, R, (int64_t)S.n * C.heads * p.groups);
+    KMQ_LAUNCH_CHECK("kv_weigh");
+  }
   return KM_OK;
 }
 

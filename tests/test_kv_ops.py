@@ -157,7 +157,7 @@ def test_four_bits_want_multiples_of_32(kmq):
         c, s, r = (ct.byref(x) for x in _args(kmq, dict(d=d)))
         for st in (L.kv_write(c, s, r, r, 1, None), L.kv_read(c, s, r, r, 1, None),
                    L.kv_attend(c, s, r, 4, 0.1, 1, 0, r, 1, None, None, 0, None), L.kv_attend_bytes(c, s, 4, 1, 0, 1),
-                   L.kv_weigh(c, s, r, 4, 0.1, 1, 0, 1, FAKE, FAKE, 1.0, None), L.kv_evict_bytes(c, s, 5)):
+                   L.kv_weigh(c, s, r, 4, 0.1, 1, 0, 1, FAKE, FAKE, 1.0, None, 0, None), L.kv_weigh_bytes(c, s, 4, 1, 0, 1), L.kv_evict_bytes(c, s, 5)):
             assert st == -1 and "multiple of 32" in L.km_last_error().decode()
     for d in (32, 96, 256):
         c, s, r = (ct.byref(x) for x in _args(kmq, dict(d=d)))
@@ -204,9 +204,13 @@ def test_weigh_refusals(kmq):
     L = kmq.lib()
     c, s, r = _args(kmq)
 
-    def call(cache=c, seqs=s, q=r, hq=4, scale=0.1, flags=1, window=0, type_=1, lse=FAKE, weight=FAKE, decay=1.0):
+    def call(cache=c, seqs=s, q=r, hq=4, scale=0.1, flags=1, window=0, type_=1, lse=FAKE, weight=FAKE, decay=1.0, ws=None, n=0):
         p = [None if x is None else ct.byref(x) for x in (cache, seqs, q)]
-        return L.kv_weigh(p[0], p[1], p[2], hq, scale, flags, window, type_, lse, weight, decay, None)
+        return L.kv_weigh(p[0], p[1], p[2], hq, scale, flags, window, type_, lse, weight, decay, ws, n, None)
+
+    prompt = _args(kmq, seqs=dict(n=1, max_rows=2000, rows=2000, max_pages=40, table_ld=40))[1]
+    need = L.kv_weigh_bytes(ct.byref(c), ct.byref(prompt), 4, 1, 0, 1)
+    assert need > 0 and L.kv_weigh_bytes(ct.byref(c), ct.byref(s), 4, 1, 0, 1) == 0
 
     for kw, status, msg in [
         (dict(cache=None), -1, "NULL"), (dict(seqs=None), -1, "NULL"), (dict(q=None), -1, "q is NULL"), (dict(lse=None), -1, "NULL"),
@@ -215,6 +219,9 @@ def test_weigh_refusals(kmq):
         (dict(decay=float("inf")), -1, "decay"), (dict(flags=2), -1, "flags"), (dict(window=-1), -1, "window"),
         (dict(flags=0, window=4), -1, "window"), (dict(type_=9), -2, "type"),
         (dict(seqs=_args(kmq, seqs=dict(table_ld=0))[1]), -1, "share"),
+        (dict(seqs=prompt, ws=FAKE, n=need - 1), -1, "ws"), (dict(seqs=prompt, ws=FAKE + 8, n=need), -1, "ws"),
+        (dict(seqs=_args(kmq, seqs=dict(n=1 << 20, rows=1 << 20))[1]), -1, "n * heads"),
+        (dict(cache=_args(kmq, dict(k_scale=0x30004))[0]), -1, "scales"),
         (dict(seqs=_args(kmq, seqs=dict(n=1, max_rows=1 << 28, rows=1 << 28, table_ld=0))[1], hq=8), -1, "2^30"),
     ]:
         assert call(**kw) == status, kw
