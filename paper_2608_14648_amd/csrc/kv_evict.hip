@@ -44,9 +44,63 @@ __device__ __forceinline__ uint32_t weight_key(float w, bool whole) {
   return whole ? 0xffffffffu : k;
 }
 
-struct Count2 {
-  int more, same;
-};
+// The K that a sequence keeps, 0 where it is left as it is, and what does not wait for the choice: the new length, the empty places of
+// kept, no page moved.  All kept: their places.  Returns whether there is something to choose.
+__device__ __forceinline__ bool select_begin(const EvictArgs &P, int b, int h, int *len, int *K) {
+  const KvCache &C = P.C;
+  const KvEvict &E = P.E;
+  const int t = threadIdx.x;
+  const int *table = P.S.table + (int64_t)b * P.S.table_ld;
+  int *kept = E.kept + ((int64_t)b * C.heads + h) * E.max_keep;
+  int *moved = P.moved + ((int64_t)b * C.heads + h) * P.tiles;
+  bool fits = evict_len(C, P.S, b, len);
+  if (fits) {
+    bool gone = false;
+    for (int p = t; p < (*len + C.page - 1) >> C.shift; p += kSelect) gone = gone || table[p] < 0 || table[p] >= C.pages;
+    fits = !__syncthreads_or(gone);
+  }
+  *K = fits ? min(*len, max(0, min(E.keep[b], E.max_keep))) : 0;
+  if (h == 0 && t == 0) E.lens[b] = fits ? *K : *len;
+  for (int i = t; i < P.tiles; i += kSelect) moved[i] = 0;
+  for (int i = *K + t; i < E.max_keep; i += kSelect) kept[i] = -1;
+  if (*K < *len) return *K > 0;
+  for (int i = t; i < *K; i += kSelect) kept[i] = i;
+  return false;
+}
+
+// Of bins counters: the digit in which the left-th largest lies, and how many are left to take of it.
+__device__ __forceinline__ void find_digit(const uint32_t *hist, int bins, int *digit, int *left, int *wave_sum, uint32_t *found) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int each = bins / kSelect;  // 2 or 1: thread t has digits bins - 1 - each * t and the ones below it
+  int mine = 0;
+  for (int i = 0; i < each; ++i) mine += (int)hist[bins - 1 - each * t - i];
+  int sum = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const int y = __shfl_up(sum, o);
+    if (lane >= o) sum += y;
+  }
+  if (lane == 63) wave_sum[wave] = sum;
+  __syncthreads();
+  int above = sum - mine;
+  for (int y = 0; y < wave; ++y) above += wave_sum[y];
+  if (above < *left && above + mine >= *left) {
+    int i = 0;
+    for (; i < each - 1; ++i) {
+      const int n = (int)hist[bins - 1 - each * t - i];
+      if (above + n >= *left) break;
+      above += n;
+    }
+    found[0] = (uint32_t)(bins - 1 - each * t - i);
+    found[1] = (uint32_t)(*left - above);
+  }
+  __syncthreads();
+  *digit = (int)found[0];
+  *left = (int)found[1];
+  __syncthreads();  // before wave_sum and found are written again
+}
+
+__device__ constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
 
 __global__ __launch_bounds__(kSelect) void kv_select_kernel(EvictArgs P) {
   __shared__ uint32_t hist[kBins];
@@ -59,22 +113,8 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(EvictArgs P) {
   int *kept = E.kept + ((int64_t)b * C.heads + h) * E.max_keep;
   int *moved = P.moved + ((int64_t)b * C.heads + h) * P.tiles;
   const int *table = P.S.table + (int64_t)b * P.S.table_ld;
-  int len;
-  bool fits = evict_len(C, P.S, b, &len);
-  if (fits) {
-    bool gone = false;
-    for (int p = t; p < (len + C.page - 1) >> C.shift; p += kSelect) gone = gone || table[p] < 0 || table[p] >= C.pages;
-    fits = !__syncthreads_or(gone);
-  }
-  const int K = fits ? min(len, max(0, min(E.keep[b], E.max_keep))) : 0;
-  if (h == 0 && t == 0) E.lens[b] = fits ? K : len;
-  for (int i = t; i < P.tiles; i += kSelect) moved[i] = 0;
-  for (int i = K + t; i < E.max_keep; i += kSelect) kept[i] = -1;
-  if (K == 0) return;
-  if (K == len) {
-    for (int i = t; i < K; i += kSelect) kept[i] = i;
-    return;
-  }
+  int len, K;
+  if (!select_begin(P, b, h, &len, &K)) return;
   // a thread's next positions j .. j + 7 lie in one page
   auto keys = [&](int j, uint32_t *k) {
     const int pg = table[j >> C.shift];
@@ -86,10 +126,9 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(EvictArgs P) {
   };
   uint32_t prefix = 0;
   int left = K;  // how many to take of the keys that begin with prefix
-  constexpr int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
-    const int shift = shifts[pass], bins = 1 << bits[pass];
+    const int shift = kShift[pass], bins = 1 << kBits[pass];
     for (int i = t; i < bins; i += kSelect) hist[i] = 0;
     __syncthreads();
     for (int j = kOwn * t; j < len; j += kOwn * kSelect) {
@@ -97,37 +136,12 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(EvictArgs P) {
       keys(j, k);
 #pragma unroll
       for (int i = 0; i < kOwn; ++i)
-        if (j + i < len && (pass == 0 || k[i] >> (shift + bits[pass]) == prefix)) atomicAdd(&hist[(k[i] >> shift) & (bins - 1)], 1u);
+        if (j + i < len && (pass == 0 || k[i] >> (shift + kBits[pass]) == prefix)) atomicAdd(&hist[(k[i] >> shift) & (bins - 1)], 1u);
     }
     __syncthreads();
-    // from the largest digit down: thread t has digits bins - 1 - each * t and the ones below it
-    const int each = bins / kSelect;  // 2 or 1
-    int mine = 0;
-    for (int i = 0; i < each; ++i) mine += (int)hist[bins - 1 - each * t - i];
-    int sum = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const int y = __shfl_up(sum, o);
-      if (lane >= o) sum += y;
-    }
-    if (lane == 63) wave_a[wave] = sum;
-    __syncthreads();
-    int above = sum - mine;
-    for (int y = 0; y < wave; ++y) above += wave_a[y];
-    if (above < left && above + mine >= left) {
-      int i = 0;
-      for (; i < each - 1; ++i) {
-        const int n = (int)hist[bins - 1 - each * t - i];
-        if (above + n >= left) break;
-        above += n;
-      }
-      found[0] = (uint32_t)(bins - 1 - each * t - i);
-      found[1] = (uint32_t)(left - above);
-    }
-    __syncthreads();
-    prefix = (prefix << bits[pass]) | found[0];
-    left = (int)found[1];
-    __syncthreads();  // before hist, wave_a and found are written again
+    int digit;
+    find_digit(hist, bins, &digit, &left, wave_a, found);
+    prefix = (prefix << kBits[pass]) | (uint32_t)digit;
   }
   // those above the key `prefix`, and the first `left` of those equal to it, in the order of positions
   int more0 = 0, same0 = 0;
@@ -182,6 +196,166 @@ __global__ __launch_bounds__(kSelect) void kv_select_kernel(EvictArgs P) {
     }
     __syncthreads();
   }
+}
+
+// ---- few long sequences: the same with `slices` workgroups to a sequence's head, a kernel for each pass -------------------
+
+struct SelectArgs {
+  EvictArgs E;
+  int slices;
+  uint32_t *hist;  // [n * heads][3][kBins], counters of all slices
+  int *ends;       // [n * heads][slices][2]: keys above the threshold and equal to it, of each slice
+  int *state;      // [n * heads][2]: length, K; 0, 0: nothing to choose
+};
+
+__global__ __launch_bounds__(kSelect) void kv_select_begin_kernel(SelectArgs P) {
+  const int bh = (int)blockIdx.x, h = bh % P.E.C.heads, b = bh / P.E.C.heads, t = threadIdx.x;
+  int len, K;
+  const bool some = select_begin(P.E, b, h, &len, &K);
+  if (t < 2) P.state[2 * bh + t] = !some ? 0 : t ? K : len;
+  for (int i = t; i < 3 * kBins; i += kSelect) P.hist[(int64_t)bh * 3 * kBins + i] = 0;
+}
+
+// PASS 0, 1, 2: counts a digit of the slice's keys.  3: counts its keys above the threshold and equal to it.  4: writes who stays.
+template <int PASS>
+__global__ __launch_bounds__(kSelect) void kv_select_slice_kernel(SelectArgs P) {
+  constexpr int kCopies = 4;  // of each counter, for every fourth lane: lanes that count the same digit wait for each other
+  __shared__ uint32_t hist[PASS < 3 ? kBins * kCopies : kSelect / 64 * 2];
+  __shared__ int wave_sum[kSelect / 64];
+  __shared__ uint32_t found[2];
+  const KvCache &C = P.E.C;
+  const KvEvict &E = P.E.E;
+  const int bh = (int)(blockIdx.x / (uint32_t)P.slices), slice = (int)(blockIdx.x - (uint32_t)bh * P.slices);
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int len = P.state[2 * bh], K = P.state[2 * bh + 1];
+  if (K == 0) return;
+  const int h = bh % C.heads, b = bh / C.heads;
+  const int *table = P.E.S.table + (int64_t)b * P.E.S.table_ld;
+  // this slice's positions [s0, s1); each wave has a run of them, 256 at a time
+  constexpr int kStep = 4 * 64;
+  const int64_t each = cdiv(cdiv(len, P.slices), kStep * (kSelect / 64)) * kStep * (kSelect / 64);
+  const int64_t s0 = min(each * slice, (int64_t)len), s1 = min(s0 + each, (int64_t)len);
+  const int64_t r0 = min(s0 + each / (kSelect / 64) * wave, s1), r1 = min(r0 + each / (kSelect / 64), s1);
+  uint32_t prefix = 0;
+  int left = K;
+  uint32_t *all = P.hist + (int64_t)bh * 3 * kBins;
+#pragma unroll
+  for (int y = 0; y < (PASS < 3 ? PASS : 3); ++y) {
+    int digit;
+    find_digit(all + y * kBins, 1 << kBits[y], &digit, &left, wave_sum, found);
+    prefix = (prefix << kBits[y]) | (uint32_t)digit;
+  }
+  // the weights of positions j .. j + 3, which lie in one page; behind the end those of the last four
+  auto load = [&](int64_t j) {
+    const int at = (int)min(j, (int64_t)((len - 1) & ~3));
+    const int pg = table[at >> C.shift];
+    return *reinterpret_cast<const f32x4 *>(E.weight + ((int64_t)pg * C.heads + h) * C.page + (at & (C.page - 1)));
+  };
+  auto key = [&](const f32x4 &w, int64_t j, int i) { return weight_key(w[i], j + i < E.first || j + i >= len - E.recent); };
+  // f(weights, first position) for this wave's run, with the loads of four steps on their way
+  auto each_step = [&](auto f) {
+    for (int64_t j0 = r0 + 4 * lane; j0 - 4 * lane < r1; j0 += 4 * kStep) {
+      f32x4 w[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) w[y] = load(j0 + y * kStep);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) f(w[y], j0 + y * kStep);
+    }
+  };
+  if constexpr (PASS < 3) {
+    constexpr int shift = kShift[PASS], bins = 1 << kBits[PASS];
+    for (int i = t; i < bins * kCopies; i += kSelect) hist[i] = 0;
+    __syncthreads();
+    each_step([&](const f32x4 &w, int64_t j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t k = key(w, j, i);
+        if (j + i < r1 && (PASS == 0 || k >> (shift + kBits[PASS]) == prefix))
+          atomicAdd(&hist[((k >> shift) & (bins - 1)) * kCopies + (lane & (kCopies - 1))], 1u);
+      }
+    });
+    __syncthreads();
+    for (int i = t; i < bins; i += kSelect) {
+      const uint32_t n = hist[4 * i] + hist[4 * i + 1] + hist[4 * i + 2] + hist[4 * i + 3];
+      if (n) atomicAdd(&all[PASS * kBins + i], n);  // whole numbers: in any order the same
+    }
+    return;
+  }
+  int more = 0, same = 0;
+  each_step([&](const f32x4 &w, int64_t j) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t k = key(w, j, i);
+      more += j + i < r1 && k > prefix;
+      same += j + i < r1 && k == prefix;
+    }
+  });
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    more += __shfl_xor(more, o);
+    same += __shfl_xor(same, o);
+  }
+  if (lane == 0) {
+    hist[2 * wave] = (uint32_t)more;
+    hist[2 * wave + 1] = (uint32_t)same;
+  }
+  __syncthreads();
+  int *ends = P.ends + (int64_t)bh * P.slices * 2;
+  if constexpr (PASS == 3) {
+    if (t < 2) {
+      int n = 0;
+      for (int y = 0; y < kSelect / 64; ++y) n += (int)hist[2 * y + t];
+      ends[2 * slice + t] = n;
+    }
+    return;
+  }
+  // what comes before this wave's run
+  more = same = 0;
+  for (int y = lane; y < slice; y += 64) {
+    more += ends[2 * y];
+    same += ends[2 * y + 1];
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    more += __shfl_xor(more, o);
+    same += __shfl_xor(same, o);
+  }
+  for (int y = 0; y < wave; ++y) {
+    more += (int)hist[2 * y];
+    same += (int)hist[2 * y + 1];
+  }
+  int *kept = E.kept + (int64_t)bh * E.max_keep;
+  int *moved = P.E.moved + (int64_t)bh * P.E.tiles;
+  each_step([&](const f32x4 &w, int64_t j) {
+    uint32_t k[4];
+    int here = 0;  // both counts, 16 bits each
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      k[i] = key(w, j, i);
+      here += j + i < r1 ? (k[i] > prefix) + (k[i] == prefix ? 1 << 16 : 0) : 0;
+    }
+    int sum = here;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int y = __shfl_up(sum, o);
+      if (lane >= o) sum += y;
+    }
+    int m = more + ((sum - here) & 0xffff), e = same + ((sum - here) >> 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool up = j + i < r1 && k[i] > prefix, eq = j + i < r1 && k[i] == prefix;
+      if (up || (eq && e < left)) {
+        const int at = m + min(e, left);
+        kept[at] = (int)(j + i);
+        if (at != j + i) moved[at >> C.shift] = 1;
+      }
+      m += up;
+      e += eq;
+    }
+    const int both = __shfl(sum, 63);
+    more += both & 0xffff;
+    same += both >> 16;
+  });
 }
 
 struct EvictTile {
@@ -336,23 +510,33 @@ int tiles_of(const KvCache &C, const KvSeqs &S, int max_keep) {
   return (int)std::min<int64_t>(S.max_pages, cdiv(max_keep, C.page));
 }
 
+// Workgroups that choose for a sequence's head: one, but for few long sequences.  One takes about 1 us per thousand positions in all
+// of its passes and 8 more (one sequence of 100001 tokens, 8 heads: 85 us); five kernels take 25.
+int slices_of(const KvCache &C, const KvSeqs &S) {
+  const int64_t heads = (int64_t)S.n * C.heads;
+  return S.max_len > 24576 && heads <= 128 ? (int)std::min(cdiv(S.max_len, 8192), 512 / heads) : 1;
+}
+
 // Bytes of each part of the workspace, 16-byte aligned.
 struct Parts {
-  size_t moved, codes, scales, weights;
+  size_t moved, codes, scales, weights, hist, ends, state;
 };
 Parts parts_of(const KvCache &C, const KvSeqs &S, int max_keep) {
   auto up = [](size_t x) { return (x + 15) & ~(size_t)15; };
   const size_t slots = (size_t)S.n * C.heads * tiles_of(C, S, max_keep);
   const bool i4 = C.fmt == KM_KV_I4;
-  return {up(4 * slots), up(2 * slots * C.page * C.d / (i4 ? 2 : 1)), up(8 * slots * (i4 ? C.page : 1)),
-          up(4 * slots * C.page)};
+  const int slices = slices_of(C, S);
+  const size_t heads = slices > 1 ? (size_t)S.n * C.heads : 0;
+  return {up(4 * slots),        up(2 * slots * C.page * C.d / (i4 ? 2 : 1)), up(8 * slots * (i4 ? C.page : 1)),
+          up(4 * slots * C.page), 4 * heads * 3 * kBins,                       up(8 * heads * slices),
+          up(8 * heads)};
 }
 
 }  // namespace
 
 size_t kv_evict_scratch(const KvCache &C, const KvSeqs &S, int max_keep) {
   const Parts p = parts_of(C, S, max_keep);
-  return p.moved + p.codes + p.scales + p.weights;
+  return p.moved + p.codes + p.scales + p.weights + p.hist + p.ends + p.state;
 }
 
 int64_t kv_evict_blocks(const KvCache &C, const KvSeqs &S, int max_keep) {
@@ -364,7 +548,20 @@ km_status launch_kv_evict(const KvCache &C, const KvSeqs &S, const KvEvict &E, v
   uint8_t *w = static_cast<uint8_t *>(ws);
   EvictArgs P{C, S, E, tiles_of(C, S, E.max_keep), reinterpret_cast<int *>(w), w + p.moved,
               reinterpret_cast<float *>(w + p.moved + p.codes), reinterpret_cast<float *>(w + p.moved + p.codes + p.scales), 0};
-  kv_select_kernel<<<dim3((unsigned)(S.n * C.heads)), kSelect, 0, s>>>(P);
+  const unsigned heads = (unsigned)(S.n * C.heads);
+  if (const int slices = slices_of(C, S); slices > 1) {
+    w += p.moved + p.codes + p.scales + p.weights;
+    const SelectArgs A{P, slices, reinterpret_cast<uint32_t *>(w), reinterpret_cast<int *>(w + p.hist),
+                       reinterpret_cast<int *>(w + p.hist + p.ends)};
+    kv_select_begin_kernel<<<dim3(heads), kSelect, 0, s>>>(A);
+    kv_select_slice_kernel<0><<<dim3(heads * slices), kSelect, 0, s>>>(A);
+    kv_select_slice_kernel<1><<<dim3(heads * slices), kSelect, 0, s>>>(A);
+    kv_select_slice_kernel<2><<<dim3(heads * slices), kSelect, 0, s>>>(A);
+    kv_select_slice_kernel<3><<<dim3(heads * slices), kSelect, 0, s>>>(A);
+    kv_select_slice_kernel<4><<<dim3(heads * slices), kSelect, 0, s>>>(A);
+  } else {
+    kv_select_kernel<<<dim3(heads), kSelect, 0, s>>>(P);
+  }
   KMQ_LAUNCH_CHECK("kv_evict");
   const int64_t blocks = kv_evict_blocks(C, S, E.max_keep), most = kv_piece(kGather);
   auto go = [&](auto *kernel) {

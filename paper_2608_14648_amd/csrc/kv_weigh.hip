@@ -300,10 +300,12 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
   uint32_t x = P.block0 + blockIdx.x;
   const int h = (int)(x % (uint32_t)C.heads);  // heads fastest: a head's workgroups share an XCD's L2 where they are a multiple of 8
   x /= (uint32_t)C.heads;
-  const int b = (int)(x % (uint32_t)P.S.n);
-  x /= (uint32_t)P.S.n;
-  // the first positions, which most rows see, begin first
-  const int split = (int)(x % (uint32_t)R.splits), group0 = (int)(x / (uint32_t)R.splits);
+  // Neighbouring workgroups of an XCD go to its shader engines in turn, whatever these still have to do: splits, which are alike,
+  // follow each other, then the sequences (sequences first, of 5340 and 3133 tokens: two of four engines had all of the longer one's,
+  // 347 us).  The first positions, which most rows see, begin first.
+  const int split = (int)(x % (uint32_t)R.splits);
+  x /= (uint32_t)R.splits;
+  const int b = (int)(x % (uint32_t)P.S.n), group0 = (int)(x / (uint32_t)P.S.n);
   KvSeq q;
   if (!kv_seq(P.S, C.page, b, &q) || q.n == 0) return;
   const bool parts = weigh_split(R, q);
@@ -322,8 +324,12 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
   const KvNibbles nib = kv_nibbles();
   const int per = d / 8;  // pieces of a row
   int prow[NI];
+  int64_t q_at[NI];  // from a tile's first token
 #pragma unroll
-  for (int i = 0; i < NI; ++i) prow[i] = (t + i * T) / per;
+  for (int i = 0; i < NI; ++i) {
+    prow[i] = (t + i * T) / per;
+    q_at[i] = prow[i] * A.q.row + 8 * (t + i * T - prow[i] * per);
+  }
 
   for (int64_t gi = group0; gi * kRowKeys < q.len; gi += P.groups) {
     const int w0 = (int)gi * kRowKeys, j0 = w0 + wave * kChunk;
@@ -380,47 +386,44 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
     const int64_t tiles = (int64_t)nb * A.group, ns = parts ? R.splits : 1;
     const int z0 = (int)(tiles * split / ns), z1 = (int)(tiles * (split + 1) / ns);
     int lh = nb ? z0 / nb : 0, lb = b0 + z0 - lh * nb;  // head and block of the tile that is loaded next
-    u32x4 raw[NI];
-    float lse[NI];
-    auto load = [&] {
+    u32x4 raw[1][NI];
+    float lse[1];  // of token t, in the first half of a wave
+    auto load = [&](int to) {
       const int64_t row = q.row0 + (int64_t)lb * kRowTile;
       const uint16_t *base = static_cast<const uint16_t *>(A.q.p) + row * A.q.row + (int64_t)(h * A.group + lh) * A.q.head;
-      const int left = q.n - lb * kRowTile;
+      const int left = min(q.n - lb * kRowTile, kRowTile);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const bool in = prow[i] < min(left, kRowTile);
-        const int r = in ? prow[i] : 0, c = in ? t + i * T - r * per : 0;
-        raw[i] = *reinterpret_cast<const u32x4 *>(base + r * A.q.row + 8 * c);
-        lse[i] = in ? A.lse[(row + r) * C.heads * A.group + h * A.group + lh] : INFINITY;
+        const bool in = prow[i] < left;
+        raw[to][i] = *reinterpret_cast<const u32x4 *>(base + (in ? q_at[i] : 0));
       }
+      if (t < kRowTile) lse[to] = t < left ? A.lse[(row + t) * C.heads * A.group + h * A.group + lh] : INFINITY;
       if (++lb == b1) {
         lb = b0;
         ++lh;
       }
     };
-    auto store = [&](int z) {
+    auto store = [&](int z, int from) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         if (prow[i] >= kRowTile) continue;
-        const bool counts = fabsf(lse[i]) < INFINITY;  // rows that do not count may hold NaN
-        const int c = t + i * T - prow[i] * per;
-        *reinterpret_cast<u32x4 *>(&qt[z & 1][prow[i] * LD + 16 * c]) = counts ? raw[i] : u32x4{0, 0, 0, 0};
-        if (c == 0) stat[z & 1][prow[i]] = counts ? -lse[i] * kLog2e : -INFINITY;
+        *reinterpret_cast<u32x4 *>(&qt[z & 1][prow[i] * LD + 16 * (t + i * T - prow[i] * per)]) = raw[from][i];
       }
+      if (t < kRowTile) stat[z & 1][t] = fabsf(lse[from]) < INFINITY ? -lse[from] * kLog2e : -INFINITY;
     };
     float sum[32];
 #pragma unroll
     for (int e = 0; e < 32; ++e) sum[e] = 0.0f;
     int cb = lb;  // block of the tile at hand
     if (z0 < z1) {
-      load();
-      store(z0);
-      if (z0 + 1 < z1) load();
+      load(0);
+      store(z0, 0);
+      if (z0 + 1 < z1) load(0);
       __syncthreads();
     }
     for (int z = z0; z < z1; ++z) {
-      if (z + 1 < z1) store(z + 1);
-      if (z + 2 < z1) load();
+      if (z + 1 < z1) store(z + 1, 0);
+      if (z + 2 < z1) load(0);
       const int pos0 = first + cb * kRowTile;  // position of the tile's first token
       if (mine && (!A.causal || pos0 + kRowTile > j0) && (!A.window || (int64_t)pos0 < (int64_t)j0 + kChunk - 1 + A.window)) {
         f32x16v s[2];
@@ -442,6 +445,10 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
           }
         }
         const float nl = stat[z & 1][m];
+        if (__any(nl == -INFINITY)) {  // rows that do not count may hold NaN
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] = nl == -INFINITY ? 0.0f : s[e >> 4][e & 15];
+        }
         const int pos = pos0 + m;
         const int see0 = A.window ? max(pos + 1 - A.window, 0) : 0, see1 = A.causal ? max(pos + 1, 0) : q.len;
         if (!__all(j0 >= see0 && j0 + kChunk <= see1)) {
