@@ -271,6 +271,148 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !
 }
 
 
+// ---- up to 16 rows to a cache head: single tokens ---------------------------------------------------------------------------------
+//
+// The rows stay in registers, scaled to fp16 as in kv_attend.hpp, and a wave goes through chunks of 64 positions, the next one's codes
+// and weights on their way meanwhile.
+template <int FMT, int NS, int NP, bool ONE>
+__global__ __launch_bounds__(64 * kFewWaves, NP <= 2 && NS == 1 ? 4 : 2) void kv_weigh_tokens_kernel(WeighArgs P) {
+  const KvCache &C = P.C;
+  const KvAttend &A = P.A;
+  uint32_t x = P.block0 + blockIdx.x;
+  const int h = (int)(x % (uint32_t)C.heads);  // heads fastest: a head's workgroups share an XCD's L2 where they are a multiple of 8
+  x /= (uint32_t)C.heads;
+  const int group = (int)(x % (uint32_t)P.groups), b = (int)(x / (uint32_t)P.groups);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+  KvSeq q;
+  if (!kv_seq(P.S, C.page, b, &q) || q.n == 0) return;
+  const int d = C.d, rows = q.n * A.group, chunks = (int)cdiv(q.len, kChunk), step = P.groups * kFewWaves;
+  const KvNibbles nib = kv_nibbles();
+  const int64_t hb = kv_bytes<FMT>((int64_t)C.page * d);
+  const int db = (int)kv_bytes<FMT>(d);
+  const int pmask = C.page - 1, last = max(q.len - 1, 0), kr = m >> 2, ktok = m & 3;
+  const int *table = P.S.table + (int64_t)b * P.S.table_ld;
+  auto page_of = [&](int j) {
+    const int pg = table[min(j, last) >> C.shift];
+    return ONE ? __builtin_amdgcn_readfirstlane(pg) : pg;
+  };
+  auto there_at = [&](int pg) { return pg >= 0 && pg < C.pages; };
+  auto head_at = [&](int pg) { return (int64_t)(there_at(pg) ? pg : 0) * C.heads + h; };
+  int pk, pv;
+  auto pages = [&](int c) {
+    pv = page_of(c * kChunk + (ONE ? 0 : 16 * g));
+    pk = ONE ? pv : page_of(c * kChunk + 16 * kr);
+  };
+  Codes16<FMT> kw[4][NP];
+  float ks, old;  // 4-bit codes: scale of position m of run g; weight of that position
+  bool mine;
+  int64_t at;
+  auto load_keys = [&](int c) {
+    const uint8_t *kp = C.k + head_at(pk) * hb + ((c * kChunk + (ONE ? 0 : 16 * kr)) & pmask) * db;
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        kw[st][p] = *reinterpret_cast<const Codes16<FMT> *>(
+            kp + 4 * st * db + (uint32_t)(((ONE ? 16 * kr : 0) + ktok) * db + (int)kv_bytes<FMT>(min(64 * p + 16 * g, d - 16))));
+  };
+  auto load_rest = [&](int c) {
+    const int j = c * kChunk + 16 * g + m;
+    const bool there = there_at(pv);
+    mine = there && j < q.len;
+    at = head_at(pv) * C.page + (j & pmask);
+    old = mine && P.decay != 0.0f && j < q.len - q.n ? P.weight[at] : 0.0f;
+    if constexpr (FMT == KM_KV_I4) ks = mine ? C.ks[at] : 1.0f;
+    else ks = there && c * kChunk + 16 * g < q.len ? C.ks[head_at(pv)] : 1.0f;
+  };
+  int c = group * kFewWaves + wave;
+  if (c >= chunks) return;  // no barrier follows
+  pages(c);
+  load_keys(c);
+  load_rest(c);
+  if (c + step < chunks) pages(c + step);
+
+  // this lane's row, its statistics and its span; rows behind the last and rows that do not count add nothing
+  const int r = min(m, rows - 1);
+  const RowAt row = row_at(A, C, q, h, r);
+  int lo, hi;
+  row_span(A, q, r, &lo, &hi);
+  u32x4 raw[NP][2 * NS];
+  const char *qp = static_cast<const char *>(A.q.p) + row.q * (2 * NS);
+#pragma unroll
+  for (int p = 0; p < NP; ++p)
+#pragma unroll
+    for (int i = 0; i < 2 * NS; ++i) raw[p][i] = reinterpret_cast<const u32x4 *>(qp + 2 * NS * min(64 * p + 16 * g, d - 16))[i];
+  const float lse = A.lse[row.lse];
+  const bool counts = m < rows && fabsf(lse) < INFINITY;
+  const float nl = counts ? -lse * kLog2e : -INFINITY;
+  f16x8 qf[NP][2][NS];
+  float cs;
+  {
+    float top = 0.0f, f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) top = fmaxf(top, top16<NS>(raw[p], A.type));
+    q_scale(max_groups(top), A.scale, &f, &cs);
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      float v[16];
+      values16<NS>(raw[p], A.type, v);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = counts && 64 * p + 16 * g < d ? v[i] * f : 0.0f;  // rows that do not count may hold NaN
+        const _Float16 y16 = (_Float16)y;
+        qf[p][i / 8][0][place8<FMT>(i % 8)] = y16;
+        if constexpr (NS == 2) qf[p][i / 8][1][place8<FMT>(i % 8)] = (_Float16)(y - (float)y16);
+      }
+    }
+  }
+  if (!counts) cs = 1.0f;
+
+  for (; c < chunks; c += step) {
+    const int j0 = c * kChunk;
+    const bool more = c + step < chunks;
+    f32x4 s[4];
+#pragma unroll
+    for (int st = 0; st < 4; ++st) {
+      __builtin_amdgcn_sched_barrier(0);  // no more codes widened at a time than these products take
+      s[st] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const f16x8 kf = widen8<FMT>(kw[st][p], k, nib);
+#pragma unroll
+          for (int z = 0; z < NS; ++z) s[st] = mfma16(kf, qf[p][k][z], s[st]);
+        }
+    }
+    if (more) load_keys(c + step);
+    if (!__all(j0 >= lo && j0 + kChunk <= hi)) {
+      int jg = j0 + 16 * g;
+      asm volatile("" : "+v"(jg));  // a branch: few chunks need it, so nothing of it is kept in registers
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int j = jg + e;
+        if (j < lo || j >= hi) s[e / 4][e % 4] = -INFINITY;
+      }
+    }
+    // a factor of 0 (a row of tiny queries) would make NaN of -inf
+    const float ck = fmaxf(FMT == KM_KV_I4 ? cs : cs * ks, 0x1p-126f);
+    float total = 0.0f;
+    each<16>([&](auto n) {
+      constexpr int e = n;
+      float y = s[e / 4][e % 4];
+      if constexpr (FMT == KM_KV_I4) y *= kv_row_bcast<e>(ks);
+      y = sum_row(__builtin_amdgcn_exp2f(fmaf(y, ck, nl)));
+      total = m == e ? y : total;
+    });
+    if (mine) P.weight[at] = fmaf(old, P.decay, total);
+    if (more) {
+      load_rest(c + step);
+      if (c + 2 * step < chunks) pages(c + 2 * step);
+    }
+  }
+}
+
 // ---- many 16-bit rows ---------------------------------------------------------------------------------------------------
 //
 // A workgroup takes 256 positions, 64 to a wave, which stay in registers as the first operand of the 32 x 32 x 16 products, and
@@ -509,6 +651,7 @@ __global__ __launch_bounds__(256) void kv_weigh_join_kernel(WeighRows R) {
 
 // How a call is cut up.
 enum WeighWay {
+  kTokens,  // up to 16 rows to a cache head: kv_weigh_tokens_kernel
   kFew,    // each wave its own positions, all rows in turn
   kShare,  // fp32 rows: a workgroup's waves share 64 positions and take the rows in turn
   kRows    // 16-bit rows: kv_weigh_rows_kernel
@@ -520,11 +663,14 @@ struct WeighPlan {
 WeighPlan plan_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   WeighPlan p{kFew, 1, 1};
   const int64_t heads = (int64_t)S.n * C.heads, rows = (int64_t)S.max_rows * A.group;
-  if (A.type == KM_T_F32 ? rows > 64 : S.max_rows >= kRowTile) p.way = A.type == KM_T_F32 ? kShare : kRows;
+  if (rows <= 16) p.way = kTokens;
+  else if (A.type == KM_T_F32 ? rows > 64 : S.max_rows >= kRowTile) p.way = A.type == KM_T_F32 ? kShare : kRows;
   // Workgroups of a sequence's head: one for each of its pieces by the longest length that the caller knows, fewer where that is
   // more than 2^20 in all (a workgroup then takes several, as where a length is longer than was said).
   const int64_t pieces = cdiv(S.max_len, p.way == kShare ? kChunk : p.way == kRows ? kRowKeys : kChunk * kFewWaves);
   p.groups = (int)std::max<int64_t>(1, std::min(pieces, (1 << 20) / heads));
+  // as many workgroups as run at a time
+  if (p.way == kTokens) p.groups = (int)std::min<int64_t>(p.groups, cdiv(1024, heads));
   // three times as many workgroups as run at a time, of eight tiles at least
   if (p.way == kRows)
     p.splits = (int)std::max<int64_t>(1, std::min(cdiv(1536, heads * p.groups), cdiv(S.max_rows, kRowTile) * A.group / 8));
@@ -570,6 +716,13 @@ km_status launch_kv_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A, 
     case 3: KV_ONE(kv_weigh_kernel, F, T, 3, M); break;          \
     default: KV_ONE(kv_weigh_kernel, F, T, 4, M);                \
   }
+#define KV_S(F, NS)                                              \
+  switch ((int)cdiv(C.d, 64)) {                                  \
+    case 1: KV_ONE(kv_weigh_tokens_kernel, F, NS, 1); break;     \
+    case 2: KV_ONE(kv_weigh_tokens_kernel, F, NS, 2); break;     \
+    case 3: KV_ONE(kv_weigh_tokens_kernel, F, NS, 3); break;     \
+    default: KV_ONE(kv_weigh_tokens_kernel, F, NS, 4);           \
+  }
 #define KV_R(F, T)                                               \
   switch (dim_tiles32(C.d)) {                                    \
     case 2: KV_ONE(kv_weigh_rows_kernel, F, T, 2); break;        \
@@ -580,7 +733,10 @@ km_status launch_kv_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A, 
   }
   auto of_format = [&](auto fmt) {
     constexpr int F = decltype(fmt)::value;
-    if (p.way == kShare) {
+    if (p.way == kTokens) {
+      if (A.type == KM_T_F32) KV_S(F, 2)
+      else KV_S(F, 1)
+    } else if (p.way == kShare) {
       KV_P(F, KM_T_F32, true)
     } else if (p.way == kFew) {
       if (A.type == KM_T_F32) KV_P(F, KM_T_F32, false)
@@ -597,6 +753,7 @@ km_status launch_kv_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A, 
   else if (C.fmt == KM_KV_F8) of_format(std::integral_constant<int, KM_KV_F8>{});
   else of_format(std::integral_constant<int, KM_KV_I4>{});
 #undef KV_R
+#undef KV_S
 #undef KV_P
 #undef KV_ARGS
 #undef KV_ONE
