@@ -305,45 +305,58 @@ def kv_rotate(rotary: KvRotary, at: KvSeqs | torch.Tensor, q: torch.Tensor, k: t
     also how the gradient of a result becomes that of what went in.  A pair (x, y) at position p with frequency f becomes
     (x cos pf - y sin pf, x sin pf + y cos pf)."""
     if isinstance(at, KvSeqs):
-        rows, device = at.rows, at.device
+        where, seqs, positions = at, at._ref, None
     else:
         _dev(at, torch.int32, "positions", 1)
-        rows, device = at.shape[0], at.device
-    if rotary.device != device:
-        raise ValueError(f"rotary on {rotary.device}, positions on {device}")
-    where = _Rows(rows, device)
-    for t, name in ((q, "q"), (k, "k")):
-        if not (t is None and name == "k") and (not isinstance(t, torch.Tensor) or t.dim() != 3):
-            raise ValueError(f"{name} must be a tensor [rows, heads, d]")
-    d = q.shape[2]
-    if k is None and k_out is not None:
+        where, seqs, positions = _Rows(at.shape[0], at.device), None, at.data_ptr()
+    rows = where.rows
+    if rotary.device != where.device:
+        raise ValueError(f"rotary on {rotary.device}, positions on {where.device}")
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a tensor [rows, heads, d]")
+    _, q_heads, d = q.shape
+    qi = _rows_of(q, "q", where, q_heads, d)
+    dtype = q.dtype
+    if q_out is None:
+        qo_t = q.new_empty((rows, q_heads, d))
+        qo = KmKvRows(qo_t.data_ptr(), q_heads * d, d)
+    else:
+        qo_t, qo = q_out, _rows_of(q_out, "q_out", where, q_heads, d, dtype, written=True)
+    ko_t = ki = ko = None
+    k_heads = 0
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 3:
+            raise ValueError("k must be a tensor [rows, heads, d]")
+        k_heads = k.shape[1]
+        ki = _rows_of(k, "k", where, k_heads, d, dtype)
+        if k_out is None:
+            ko_t = k.new_empty((rows, k_heads, d))
+            ko = KmKvRows(ko_t.data_ptr(), k_heads * d, d)
+        else:
+            ko_t, ko = k_out, _rows_of(k_out, "k_out", where, k_heads, d, dtype, written=True)
+    elif k_out is not None:
         raise ValueError("k_out without k")
-    ins = [(q, "q", q_out)] + ([] if k is None else [(k, "k", k_out)])
-    refs, outs = [], []
-    for t, name, out in ins:
-        r = _rows_of(t, name, where, t.shape[1], d, q.dtype)
+    if rows == 0:
+        return qo_t, ko_t
+    if q_out is not None or k_out is not None:
+        _check_outputs(q, k, q_out, k_out)
+    _check(lib().kv_rotate(rotary._ref, seqs, positions, rows, ct.addressof(qi), q_heads, None if k is None else ct.addressof(ki),
+                           k_heads, ct.addressof(qo), None if k is None else ct.addressof(ko), d, _TYPES[dtype],
+                           KM_ROT_INVERSE if inverse else 0, _raw_stream(where.device.index)))
+    return qo_t, ko_t
+
+
+def _check_outputs(q, k, q_out, k_out):
+    """Rows that are written overlap none of the others, but may be the ones that they are made of."""
+    for out, own, name in ((q_out, q, "q_out"), (k_out, k, "k_out")):
         if out is None:
-            out = torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        o = _rows_of(out, name + "_out", where, t.shape[1], d, q.dtype, written=True)
-        refs.append((r, o))
-        outs.append(out)
-    for i, out in enumerate(outs):
-        if ins[i][2] is None:
             continue
-        for j, (t, name, _) in enumerate(ins):
-            same = i == j and t.data_ptr() == out.data_ptr() and t.stride() == out.stride()
-            if rows and not same and not _apart(out, t):
-                raise ValueError(f"{ins[i][1]}_out overlaps {name} and is not the same rows")
-        if i and rows and not _apart(out, outs[0]):
-            raise ValueError("q_out and k_out overlap")
-    if rows:
-        qr, kr = refs[0], refs[1] if k is not None else (None, None)
-        _check(lib().kv_rotate(rotary._ref, at._ref if isinstance(at, KvSeqs) else None,
-                               None if isinstance(at, KvSeqs) else at.data_ptr(), rows, ct.addressof(qr[0]), q.shape[1],
-                               None if k is None else ct.addressof(kr[0]), 0 if k is None else k.shape[1],
-                               ct.addressof(qr[1]), None if k is None else ct.addressof(kr[1]), d, _TYPES[q.dtype],
-                               KM_ROT_INVERSE if inverse else 0, _raw_stream(device.index)))
-    return outs[0], outs[1] if k is not None else None
+        for t, of in ((q, "q"), (k, "k")):
+            same = t is own and t is not None and t.data_ptr() == out.data_ptr() and t.stride() == out.stride()
+            if t is not None and not same and not _apart(out, t):
+                raise ValueError(f"{name} overlaps {of} and is not the same rows")
+    if q_out is not None and k_out is not None and not _apart(q_out, k_out):
+        raise ValueError("q_out and k_out overlap")
 
 
 class _Rows:

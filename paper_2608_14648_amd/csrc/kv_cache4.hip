@@ -18,21 +18,26 @@ namespace {
 constexpr int kMoveThreads = 256;
 constexpr int kAhead = 4;  // rows of a lane that are on their way at a time
 
-// Eight values' codes + 8, the first in the low half of the low byte.
-__device__ __forceinline__ uint32_t nibbles8(const float *x, float mul) {
-  uint32_t o = 0;
+// Eight values' codes + 8, a byte each, the first in the low byte.
+template <bool CLAMP>
+__device__ __forceinline__ u32x2 codes8(const float *x, float mul) {
+  uint32_t q[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float q = fminf(fmaxf(fmaf(x[i], mul, 12582920.0f), 12582913.0f), 12582927.0f);
-    o |= (__float_as_uint(q) & 15u) << (4 * i);
+    float y = fmaf(x[i], mul, 12582920.0f);
+    if constexpr (CLAMP) y = fminf(fmaxf(y, 12582913.0f), 12582927.0f);
+    q[i] = __float_as_uint(y);
   }
+  u32x2 o;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    o[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400u), 0x05040100u);
   return o;
 }
-
-// The same, a code to a byte.
-__device__ __forceinline__ u32x2 spread8(uint32_t w) {
-  const uint32_t e = w & 0x0f0f0f0fu, o = (w >> 4) & 0x0f0f0f0fu;
-  return u32x2{__builtin_amdgcn_perm(o, e, 0x05010400u), __builtin_amdgcn_perm(o, e, 0x07030602u)};
+// The same, two to a byte.
+__device__ __forceinline__ uint32_t halve8(u32x2 w) {
+  return __builtin_amdgcn_perm(w.y | (w.y >> 4), w.x | (w.x >> 4), 0x06040200u);
 }
 
 // Values of the eight codes of a dword.
@@ -42,8 +47,15 @@ __device__ __forceinline__ void values8(uint32_t w, float s, float *x) {
   for (int i = 0; i < 8; ++i) x[i] = value<TYPE>((float)((int)((w >> (4 * i)) & 15u) - 8), s);
 }
 
-__device__ __forceinline__ uint32_t row_max(uint32_t m, int lanes) {  // lanes: a power of two
-  for (int o = 1; o < lanes; o *= 2) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+// The largest of 4, 8, 16 or 32 neighbouring lanes, in each of them.
+__device__ __forceinline__ uint32_t row_max(uint32_t m, int lanes) {
+#define KV_DPP(ctrl) m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, ctrl, 0xf, 0xf, true))
+  KV_DPP(0xb1);  // the other of two, the other two of four
+  KV_DPP(0x4e);
+  if (lanes > 4) KV_DPP(0x141);  // the mirrored lane of eight, of sixteen
+  if (lanes > 8) KV_DPP(0x140);
+#undef KV_DPP
+  if (lanes > 16) m = max(m, (uint32_t)__shfl_xor((int)m, 16));
   return m;
 }
 
@@ -101,11 +113,12 @@ __global__ __launch_bounds__(kMoveThreads) void kv_write4_kernel(KvCache C, KvSe
         m = __float_as_uint((float)__builtin_bit_cast(f16x2, m).x);
       }
       const float mul = kv_mul4_of_top(__uint_as_float(m));
-      const uint32_t w = nibbles8(x, mul);
+      // products are past 7 only where the multiplier is the least that there is
+      const u32x2 w = __any(mul == 0x1p-30f) ? codes8<true>(x, mul) : codes8<false>(x, mul);
       if (!in || r >= rows) continue;
       if (c == 0) scale[r] = 1.0f / mul;
-      if (values) *reinterpret_cast<u32x2 *>(turn + (r * ld + c * 8) / 4) = spread8(w);
-      else *reinterpret_cast<uint32_t *>(dst + (j.i0 + r) * (d / 2) + c * 4) = w;
+      if (values) *reinterpret_cast<u32x2 *>(turn + (r * ld + c * 8) / 4) = w;
+      else *reinterpret_cast<uint32_t *>(dst + (j.i0 + r) * (d / 2) + c * 4) = halve8(w);
     }
   }
   if (!values) return;
@@ -172,12 +185,23 @@ __global__ __launch_bounds__(kMoveThreads) void kv_read4_kernel(KvCache C, KvSeq
   const uint8_t *src = (values ? C.v : C.k) + head * C.page * (d / 2);
   if (!values) {
     const int per = d / 8, rows = j.i1 - j.i0;
-    for (int i = t; i < rows * per; i += T) {
-      const int r = i / per, c = i - r * per;
-      const uint32_t w = there ? *reinterpret_cast<const uint32_t *>(src + (j.i0 + r) * (d / 2) + c * 4) : 0x88888888u;
-      float x[8];
-      values8<TYPE>(w, there ? scale[j.i0 + r] : 0.0f, x);
-      kv_store<TYPE, 8>(out.p, at + (int64_t)r * out.row + c * 8, x);
+    for (int i0 = t; i0 < rows * per; i0 += T * kAhead) {
+      uint32_t w[kAhead];
+      float s[kAhead];
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        const int i = min(i0 + y * T, rows * per - 1);  // without conditions, so that all are on their way
+        w[y] = *reinterpret_cast<const uint32_t *>(src + j.i0 * (d / 2) + i * 4);
+        s[y] = scale[j.i0 + i / per];
+      }
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        const int i = i0 + y * T, r = i / per, c = i - r * per;
+        if (i >= rows * per) break;
+        float x[8];
+        values8<TYPE>(there ? w[y] : 0x88888888u, there ? s[y] : 0.0f, x);
+        kv_store<TYPE, 8>(out.p, at + (int64_t)r * out.row + c * 8, x);
+      }
     }
     return;
   }
@@ -187,14 +211,18 @@ __global__ __launch_bounds__(kMoveThreads) void kv_read4_kernel(KvCache C, KvSeq
     const int g = i / (d / 4), c = 4 * (i - g * (d / 4));
     if (g * 8 >= j.i1 || g * 8 + 8 <= j.i0) continue;
     uint32_t w[4];
+    f32x4 sc[2];
 #pragma unroll
-    for (int y = 0; y < 4; ++y)
-      w[y] = there ? *reinterpret_cast<const uint32_t *>(src + ((c + y) * C.page + g * 8) / 2) : 0x88888888u;
+    for (int y = 0; y < 4; ++y) w[y] = *reinterpret_cast<const uint32_t *>(src + ((c + y) * C.page + g * 8) / 2);
+#pragma unroll
+    for (int y = 0; y < 2; ++y) sc[y] = *reinterpret_cast<const f32x4 *>(scale + g * 8 + 4 * y);
+#pragma unroll
+    for (int y = 0; y < 4; ++y) w[y] = there ? w[y] : 0x88888888u;
 #pragma unroll
     for (int z = 0; z < 8; ++z) {
       const int tok = g * 8 + z;
       if (tok < j.i0 || tok >= j.i1) continue;
-      const float s = there ? scale[tok] : 0.0f;
+      const float s = there ? sc[z / 4][z % 4] : 0.0f;
       float x[4];
 #pragma unroll
       for (int y = 0; y < 4; ++y) x[y] = value<TYPE>((float)((int)((w[y] >> (4 * z)) & 15u) - 8), s);
