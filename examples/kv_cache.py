@@ -1,10 +1,10 @@
-"""A transformer's attention layer that keeps its past in 8 bits, used as a serving program would use it.
+"""A transformer's attention layer that keeps its past in 8 or 4 bits, used as a serving program would use it.
 
 Prompts of differing lengths are written into the cache (kv_write) and attended (kv_attend) at once, then every sequence
 goes on token by token; the codes are all that is kept.  At the end the keys are read back (kv_read) as the points of
 a clustering (points_bf16, kmeans_fit): the centroids say which parts of a long context a query looks at.
 
-    python examples/kv_cache.py [--dtype fp8] [--steps 32]
+    python examples/kv_cache.py [--dtype fp8 | int4] [--steps 32]
 """
 import argparse
 import math
@@ -114,7 +114,7 @@ def main(prompts=(700, 123, 1), steps=16, heads=4, group=4, d=128, page=64, dtyp
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser()
-    ap.add_argument("--dtype", choices=["int8", "fp8"], default="int8")
+    ap.add_argument("--dtype", choices=["int8", "fp8", "int4"], default="int8")
     ap.add_argument("--steps", type=int, default=16)
     a = ap.parse_args()
-    main(steps=a.steps, dtype=torch.int8 if a.dtype == "int8" else torch.float8_e4m3fn)
+    main(steps=a.steps, dtype={"int8": torch.int8, "fp8": torch.float8_e4m3fn, "int4": torch.uint8}[a.dtype])

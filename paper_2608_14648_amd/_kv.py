@@ -379,7 +379,8 @@ def kv_weigh(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, lse: torch.Tensor, w
     head, to `weight` (float32 [pages, heads, page], in place) times decay.
 
     q, scale, causal and window are those of the kv_attend call that left lse (its log-sum-exp, float32 [rows, q_heads]).  The call's own
-    tokens begin with this sum; with decay = 0 all tokens do.  Rows whose lse is not finite add nothing."""
+    tokens begin with this sum; with decay = 0 all tokens do.  Rows whose lse is not finite add nothing.  No two sequences of a call
+    may have a page in common."""
     _same(cache, seqs)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [rows, q_heads, d]")
@@ -412,7 +413,7 @@ def kv_evict(cache: KvCache, seqs: KvSeqs, weight: torch.Tensor, keep: torch.Ten
     kept: int32 [n, heads, max_keep], the position that each kept token had (-1: none); lens: int32 [n], the sequences' new lengths,
     which the program takes over (``seqs.lens.copy_(lens)``); the pages behind them are free.  Only table and lens of seqs are
     looked at.  Tokens that come later have positions that are no longer their places in the cache: rotary positions are then given
-    to kv_rotate as such."""
+    to kv_rotate as such.  No two sequences of a call may have a page in common."""
     _same(cache, seqs)
     _weights(weight, cache)
     _dev(keep, torch.int32, "keep", 1)

@@ -209,6 +209,132 @@ def test_evict_leaves_alone(fmt):
     assert host(left).tolist() == [10, 100, 100, -1, 10 ** 6] and (host(kept)[1:] == -1).all()
 
 
+# Tables that are wide enough for sequences of 25 thousand tokens: chosen from by several workgroups, whatever the lengths are.
+WIDE = 25600
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("case", range(len(EVICTS)))
+def test_evict_in_slices(fmt, case):
+    page, heads, d, lens, keep, max_keep, first, recent = EVICTS[case]
+    say(f"kv_evict {fmt} in slices page={page} heads={heads} d={d} lens={lens} keep={keep} of {max_keep}")
+    s = _setup(fmt, page, heads, d, lens, [1] * len(lens), seed=640 + case, wide=WIDE // page)
+    w, wd = _weights(s)
+    _, left = _evict(s, w, wd, keep, max_keep, first, recent, label="first")
+    _evict(s, w, wd, [max(k // 2, 0) for k in keep], max_keep, first, recent, lens=host(left), label="second")
+
+
+def test_evict_in_slices_special_and_left_alone():
+    """Ties, NaN, infinities; lengths that do not fit and pages that are not there beside sequences of several slices."""
+    s = Setup4(16, 2, 32, [17001, 40, 100, 33, 64, 16385], [1] * 6, seed=37, wide=WIDE // 16)
+    w = s.rng.choice(np.array([0.0, -0.0, 1.0, np.nan, np.inf, -np.inf, 1e-42, -2.0, 3e38, 2.0 ** -126], np.float32),
+                     (s.cache.pages, 2, 16)).astype(np.float32)
+    w[s.table[5, :1024]] = 1.0  # all the same, but for the last
+    table = s.table.copy()
+    table[2, 6] = -1
+    lens = [17001, 40, 100, -1, 10 ** 6, 16385]
+    kept, left = _evict(s, w, s.torch.from_numpy(w).cuda(), [9000, 10, 10, 10, 10, 8200], 9000, 3, 5, table=table, lens=lens,
+                        label="slices")
+    assert host(left).tolist() == [9000, 10, 100, -1, 10 ** 6, 8200]
+
+
+def test_evict_in_slices_in_a_graph():
+    """Replayed with other weights and lengths, eager calls in between: the same as an eager call each time."""
+    torch = torch_cuda()
+    s = Setup4(64, 2, 32, [30000, 900], [1, 1], seed=39)
+    keep = torch.tensor([20000, 300], dtype=torch.int32, device="cuda")
+    wd = _weights(s)[1]
+    state = (s.cache.k, s.cache.v, s.cache.k_scale, s.cache.v_scale, wd)
+    start = [t.clone() for t in state]
+
+    def step():
+        return s.km.kv_evict(s.cache, s.seqs, wd, keep, 20000, 4, 64)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = step()
+    for i in range(3):
+        s.seqs.lens.copy_(torch.tensor([30000 - 5001 * i, 900 - i], dtype=torch.int32))
+        start[4] = _weights(s)[1]
+        out = []
+        for run in (lambda: (g.replay(), held)[1], step):
+            for t, x in zip(state, start):
+                t.copy_(x)
+            got = run()
+            torch.cuda.synchronize()
+            out.append([t.clone() for t in got + state])
+        for a, b in zip(*out):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("type_", ["f16", "f32"])
+def test_weigh_many_rows_that_see_nothing_and_absent_pages(fmt, type_):
+    """As above with rows of the other types, and more of them than one tile."""
+    s = _setup(fmt, 32, 2, 96, [0, 40, 200, 33, 70], [70] * 5, seed=10, wide=2)
+    q = s.normal((s.rows, 8, 96), type_)
+    q[70, 1] = math.nan
+    q[140, 2, 5] = math.inf
+    _weigh_check(s, q, type_, label="short")
+    table = s.table.copy()
+    table[1, :] = -1
+    table[2, 1:3] = 10 ** 6
+    table[3, 0] = -5
+    _weigh_check(s, q, type_, table=table, window=50, label="absent pages")
+
+
+@pytest.mark.parametrize("type_", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [5, 200])
+def test_weigh_rows_and_any_max_len(type_, rows):
+    """Lengths past the max_len that was given: what is split over workgroups by it is not, and the sums stay right."""
+    import oracle.kv_ops as ops
+    torch = torch_cuda()
+    s = Setup4(64, 1, 64, [1500, rows, 700], [rows] * 3, seed=17)
+    q = s.normal((s.rows, 8, 64), type_)
+    _, lse = s.km.kv_attend(s.cache, s.seqs, q, lse=True)
+    old = np.zeros((s.cache.pages, 1, 64), np.float32)
+    want, big, els = ops.weigh(s.orc, s.table, s.lens, s.starts, q.float().cpu().numpy(), host(lse), old,
+                               float(np.float32(1 / math.sqrt(64))))
+    e = 2.0 ** -24 * (64 * big + 4 * (1.45 * big + 16) + 8)
+    bound = np.abs(want) * (2 * e + rows * 8 * 2.0 ** -24 + (2.0 ** -20 * big if type_ == "f32" else 0) + 2.0 ** -23) + \
+        12 * 2.0 ** -24 * els + 1e-37
+    for max_len in (0, 300, 1500, 10 ** 9):
+        seqs = s.km.KvSeqs(s.seqs.table, s.seqs.lens, s.seqs.starts, rows=s.rows, max_rows=rows, max_len=max_len)
+        w = torch.zeros((s.cache.pages, 1, 64), device="cuda")
+        s.km.kv_weigh(s.cache, seqs, q, lse, w)
+        assert (np.abs(host(w) - want) <= bound).all(), max_len
+
+
+@pytest.mark.parametrize("rows", [1, 90])
+def test_weigh_and_evict_past_32_bits(rows):
+    """Pages behind the first 2^31 bytes of codes: as in a small cache."""
+    torch = torch_cuda()
+    import paper_2608_14648_amd as km
+    heads, page, d = 8, 128, 256  # 256 KiB of codes to a page
+    pages = (1 << 31) // (heads * page * d) + 40
+    say(f"kv_weigh and kv_evict large: {pages} pages, {rows} rows")
+    large, small = km.kv_cache(pages, heads, d, page), km.kv_cache(4, heads, d, page)
+    rng = np.random.default_rng(2)
+    x, y = (torch.from_numpy(rng.standard_normal((300, heads, d)).astype(np.float32)).bfloat16().cuda() for _ in range(2))
+    got = []
+    for c, table in ((large, [pages - 1, 5, pages - 7]), (small, [1, 0, 3])):
+        t = torch.tensor([table], dtype=torch.int32, device="cuda")
+        lens = torch.tensor([300], dtype=torch.int32, device="cuda")
+        km.kv_write(c, km.KvSeqs(t, lens, rows=300, max_rows=300), x, y)
+        seqs = km.KvSeqs(t, lens, rows=rows, max_rows=rows, max_len=300)
+        _, lse = km.kv_attend(c, seqs, x[:rows].contiguous(), lse=True)
+        w = torch.zeros((c.pages, heads, page), device="cuda")
+        km.kv_weigh(c, seqs, x[:rows].contiguous(), lse, w)
+        kept, left = km.kv_evict(c, seqs, w, torch.tensor([140], dtype=torch.int32, device="cuda"), 140, 4, 16)
+        back = km.kv_read(c, km.KvSeqs(t, left, rows=140, max_rows=140))
+        got.append((kept, left) + back + (w[torch.tensor(table[:2], device="cuda").long()][:, :, :12],))
+    torch.cuda.synchronize()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 def test_evict_long():
     """One long sequence; the order of positions and the digits of the weights."""
     torch = torch_cuda()

@@ -397,3 +397,18 @@ def test_offsets_past_32_bits():
     torch.cuda.synchronize()
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+def test_example():
+    """The example runs with 4-bit codes.  A code is off by at most half a step of a seventh of the row's largest magnitude, by the
+    root of a twelfth of a step on average; of 128 values of a normal distribution the largest is about 2.75 standard deviations (3.6
+    in nearly all rows), so keys come back within 3.6 / 7 / sqrt(12) = 15 %."""
+    torch = torch_cuda()
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "kv_cache.py")
+    spec = importlib.util.spec_from_file_location("kv_cache_example", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    r = ex.main(steps=3, dtype=torch.uint8, say=say)
+    assert r["read"] <= 0.15 and math.isfinite(r["prompt"]) and math.isfinite(r["token"])
