@@ -205,14 +205,15 @@ struct SelectArgs {
   int slices;
   uint32_t *hist;  // [n * heads][3][kBins], counters of all slices
   int *ends;       // [n * heads][slices][2]: keys above the threshold and equal to it, of each slice
-  int *state;      // [n * heads][2]: length, K; 0, 0: nothing to choose
+  int *state;      // [n * heads][8]: length, K (0, 0: nothing to choose), then prefix and left after each digit
 };
+constexpr int kState = 8;
 
 __global__ __launch_bounds__(kSelect) void kv_select_begin_kernel(SelectArgs P) {
   const int bh = (int)blockIdx.x, h = bh % P.E.C.heads, b = bh / P.E.C.heads, t = threadIdx.x;
   int len, K;
   const bool some = select_begin(P.E, b, h, &len, &K);
-  if (t < 2) P.state[2 * bh + t] = !some ? 0 : t ? K : len;
+  if (t < 2) P.state[kState * bh + t] = !some ? 0 : t ? K : len;
   for (int i = t; i < 3 * kBins; i += kSelect) P.hist[(int64_t)bh * 3 * kBins + i] = 0;
 }
 
@@ -227,7 +228,8 @@ __global__ __launch_bounds__(kSelect) void kv_select_slice_kernel(SelectArgs P) 
   const KvEvict &E = P.E.E;
   const int bh = (int)(blockIdx.x / (uint32_t)P.slices), slice = (int)(blockIdx.x - (uint32_t)bh * P.slices);
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  const int len = P.state[2 * bh], K = P.state[2 * bh + 1];
+  int *state = P.state + kState * bh;
+  const int len = state[0], K = state[1];
   if (K == 0) return;
   const int h = bh % C.heads, b = bh / C.heads;
   const int *table = P.E.S.table + (int64_t)b * P.E.S.table_ld;
@@ -239,11 +241,22 @@ __global__ __launch_bounds__(kSelect) void kv_select_slice_kernel(SelectArgs P) 
   uint32_t prefix = 0;
   int left = K;
   uint32_t *all = P.hist + (int64_t)bh * 3 * kBins;
-#pragma unroll
-  for (int y = 0; y < (PASS < 3 ? PASS : 3); ++y) {
+  if constexpr (PASS == 4) {
+    prefix = (uint32_t)state[6];
+    left = state[7];
+  } else if constexpr (PASS > 0) {  // the digit that the last kernel counted; earlier ones are known
+    constexpr int y = PASS - 1;
+    if constexpr (y > 0) {
+      prefix = (uint32_t)state[2 * y];
+      left = state[2 * y + 1];
+    }
     int digit;
     find_digit(all + y * kBins, 1 << kBits[y], &digit, &left, wave_sum, found);
     prefix = (prefix << kBits[y]) | (uint32_t)digit;
+    if (slice == 0 && t == 0) {
+      state[2 * y + 2] = (int)prefix;
+      state[2 * y + 3] = left;
+    }
   }
   // the weights of positions j .. j + 3, which lie in one page; behind the end those of the last four
   auto load = [&](int64_t j) {
@@ -259,7 +272,8 @@ __global__ __launch_bounds__(kSelect) void kv_select_slice_kernel(SelectArgs P) 
 #pragma unroll
       for (int y = 0; y < 4; ++y) w[y] = load(j0 + y * kStep);
 #pragma unroll
-      for (int y = 0; y < 4; ++y) f(w[y], j0 + y * kStep);
+      for (int y = 0; y < 4; ++y)
+        if (j0 - 4 * lane + y * kStep < r1) f(w[y], j0 + y * kStep);
     }
   };
   if constexpr (PASS < 3) {
@@ -529,7 +543,7 @@ Parts parts_of(const KvCache &C, const KvSeqs &S, int max_keep) {
   const size_t heads = slices > 1 ? (size_t)S.n * C.heads : 0;
   return {up(4 * slots),        up(2 * slots * C.page * C.d / (i4 ? 2 : 1)), up(8 * slots * (i4 ? C.page : 1)),
           up(4 * slots * C.page), 4 * heads * 3 * kBins,                       up(8 * heads * slices),
-          up(8 * heads)};
+          up(4 * heads * kState)};
 }
 
 }  // namespace
