@@ -528,7 +528,7 @@ int tiles_of(const KvCache &C, const KvSeqs &S, int max_keep) {
 // of its passes and 8 more (one sequence of 100001 tokens, 8 heads: 85 us); five kernels take 25.
 int slices_of(const KvCache &C, const KvSeqs &S) {
   const int64_t heads = (int64_t)S.n * C.heads;
-  return S.max_len > 24576 && heads <= 128 ? (int)std::min(cdiv(S.max_len, 8192), 512 / heads) : 1;
+  return S.max_len > 24576 && heads <= 128 ? (int)std::min(cdiv(S.max_len, 4096), 512 / heads) : 1;
 }
 
 // Bytes of each part of the workspace, 16-byte aligned.
