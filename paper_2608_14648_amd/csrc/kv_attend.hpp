@@ -26,6 +26,11 @@
 // 16384 tokens 176 us for 1028 MB, 5.8 TB/s, where a read alone reaches 6.3.  A chunk of a wave is about 540 vector
 // instructions, 320 of them the widening of int8 codes (five per four codes, e4m3 two), and 32 products.  16 rows of 128 dims take 208
 // registers, two waves to a SIMD; 32 rows take all 256 and spill 8 to 14 (36 to 60 bytes of scratch).
+//
+// 4-bit codes have a scale for each token: the factor ks_j and the logarithm of vs_j are brought to the lane of a position by a
+// broadcast within its sixteen, and widening takes nine instructions for eight codes.  A chunk's codes take half the registers, so
+// four-wave workgroups run three waves to a SIMD: 64 sequences of 1 to 16384 tokens 127 us for 619 MB (two waves, workgroups of eight:
+// 150), one of 131071 of 96 dims in pages of 16 30 us for 118 MB.
 #pragma once
 
 #include <type_traits>
@@ -1338,11 +1343,14 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
     //   32 rows to a tile, 64 up to 4000: 68 and 104
     // Narrower heads keep four waves: dealt out, 64 up to 16384 of 64 dims 111 us with four and 118 with eight, of 80 139 and 144,
     // of 96 162 and 160; even splits are alike, but for one head, 100000 positions: 20 and 15.
-    // Workgroups that run at a time with 128 dims, two waves to a SIMD (64 dims have room for three or four).
+    // Workgroups that run at a time with 128 dims, two waves to a SIMD (64 dims have room for three or four).  4-bit codes and 16 rows: three,
+    // which pays where tiles are dealt out (64 up to 16384: 128 us, 159 with two in workgroups of eight), elsewhere a third more
+    // pieces cost more than they gain (one sequence of 131071 40.6 us with 768, 38.9 with 512; 128 up to 4000 81 and 72), and short
+    // tiles take eight waves as the other formats do (31 up to 3000: 30.5 us with four, 25.5 with eight).
     const int64_t cap = (int64_t)S.max_pages * C.page / kChunk + 1 + kTileCost;  // whatever max_len says
     const bool three = C.fmt == KM_KV_I4 && p.nt <= 8 && p.rt == 1 && A.type != KM_T_F32;
-    const int64_t most = three ? 768 : p.nt <= 8 ? 512 : 256;
-    const bool eight = p.nt <= 8 && A.type != KM_T_F32 && !three;
+    const int64_t most = p.nt <= 8 ? 512 : 256;
+    const bool eight = p.nt <= 8 && A.type != KM_T_F32;
     p.spread = p.tiles * p.rt < 256;
     const int64_t alone = p.tiles > 256    ? 32  // the most chunks of a tile that is not split up
                           : p.tiles >= 192 ? (eight ? 96 : 48)
@@ -1357,9 +1365,9 @@ Plan plan(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
                            : std::max<int64_t>(kAttendWaves, cdiv(p.tiles * chunks, most)));
     } else {
       p.deal = 1;
-      p.wide = eight && p.nt == 8 && p.rt == 1 && chunks >= 160 && p.tiles >= 128;
+      p.wide = eight && !three && p.nt == 8 && p.rt == 1 && chunks >= 160 && p.tiles >= 128;
       p.per = 2 * (p.wide ? kWideWaves : kAttendWaves);
-      p.splits = (int)std::min<int64_t>(p.wide ? most / 2 : most, cdiv(p.tiles * chunks, p.per));
+      p.splits = (int)std::min<int64_t>(p.wide ? most / 2 : three ? 768 : most, cdiv(p.tiles * chunks, p.per));
       return p;
     }
   }

@@ -1,14 +1,17 @@
 // Eviction: each sequence and head keeps its tokens of the largest weight and closes the gaps in its pages.
 //
-// Three kernels.  kv_select_kernel, a workgroup for each sequence and head: the K-th largest weight is found digit by digit (11, 11 and
+// kv_select_kernel, a workgroup for each sequence and head: the K-th largest weight is found digit by digit (11, 11 and
 // 10 bits of the weights' ordered bit patterns, a histogram in LDS for each), then one pass in the order of positions writes down
-// who stays: all above it, and of those equal to it the first.  kv_gather_kernel, a workgroup for each page that tokens come to, keys or
+// who stays: all above it, and of those equal to it the first.  Few long sequences take several workgroups to a head and a kernel
+// for each of these passes (kv_select_slice_kernel).  kv_gather_kernel, a workgroup for each page that tokens come to, keys or
 // values: builds the page's new contents in the workspace.  kv_scatter_kernel writes them over the page.  In place at once
 // a page could be written before another has taken its tokens from it: page t takes from pages t and later.  A page whose tokens
 // all stay where they are is left out of both.
 //
-// Bound by latency for one sequence (the passes over its weights, one workgroup to a head) and by HBM for many: codes are read and
-// written twice.
+// Measured: 8 sequences of 4100 tokens, 8 heads of 128 in int8, half of them kept: 12 us to choose (latency: three passes of dependent
+// loads and counts), 35 to gather (values a byte at a time from 64-byte rows, and quotients for codes whose page had another scale: the
+// vector unit is busy half of the time), 12 to scatter (34 MB each way, 5.8 TB/s).  One sequence of 100001 tokens, 4-bit codes, 8192
+// kept: six kernels of 5 to 8 us to choose, each of them mostly its launch and a chain of three dependent loads, 15 to gather, 5 to scatter.
 #include "kv_pages.hpp"
 
 namespace kmq {
@@ -524,11 +527,13 @@ int tiles_of(const KvCache &C, const KvSeqs &S, int max_keep) {
   return (int)std::min<int64_t>(S.max_pages, cdiv(max_keep, C.page));
 }
 
-// Workgroups that choose for a sequence's head: one, but for few long sequences.  One takes about 1 us per thousand positions in all
-// of its passes and 8 more (one sequence of 100001 tokens, 8 heads: 85 us); five kernels take 25.
+// Workgroups that choose for a sequence's head: one, but for few long sequences.  One workgroup and slices, 8 heads of 128, 512 tokens
+// kept, us of a whole call: one sequence of 24000 tokens 35 and 42, of 32000 42 and 43, of 40000 47 and 41, of 100001 94 and 45; four of
+// 40000 48 and 56, of 64000 68 and 56; eight of 32000 46 and 60, of 64000 71 and 66; 16 of 64000 82 and 83, of 100001 115 and 111.
+// Slices of 8192 positions instead of 4096: one of 100001 69 instead of 65 with its pages read back.
 int slices_of(const KvCache &C, const KvSeqs &S) {
   const int64_t heads = (int64_t)S.n * C.heads;
-  return S.max_len > 24576 && heads <= 128 ? (int)std::min(cdiv(S.max_len, 4096), 512 / heads) : 1;
+  return S.max_len > 32768 + 512 * heads && heads <= 128 ? (int)std::min(cdiv(S.max_len, 4096), 512 / heads) : 1;
 }
 
 // Bytes of each part of the workspace, 16-byte aligned.

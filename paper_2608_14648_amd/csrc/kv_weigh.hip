@@ -10,9 +10,12 @@
 // formats are exact in fp16 and in bf16, so 16-bit queries are the second operand as they are; fp32 ones take two halves of fp16
 // after a power of two for each row.  The sums of a row's lane are added up over the sixteen lanes at the end.
 //
-// Few rows (one token of each sequence): each wave has its own positions; bound by the bytes of the keys.  Many rows: the
-// workgroup's waves share their 64 positions and take the row tiles in turn, since there are few positions for the number of rows; bound by
-// the exponentials (a quarter of the vector unit's rate) and the products.
+// Four ways (plan_weigh).  Single tokens: kv_weigh_tokens_kernel, bound by the bytes of the keys, 19 us for 78 MB of 16 sequences of
+// 500 to 8192 tokens in int8 (13 at the rate of a read; the longest sequence's workgroups are the last).  A few hundred rows:
+// kv_weigh_kernel, each wave with its own positions.  Prompts: kv_weigh_rows_kernel, the waves of a workgroup share tiles of rows in LDS;
+// bound by tiles (a barrier each), the products (matrix cores 25 % busy) and the exponentials (a quarter of the vector unit's rate),
+// which wait for each other: two prompts of 3133 and 5340 tokens, 4-bit codes, 220 to 250 us, 160 GFLOP.  Prompts of fp32 rows:
+// kv_weigh_kernel with a workgroup's waves sharing 64 positions and taking the rows in turn.
 #include "kv_attend.hpp"
 
 namespace kmq {
@@ -274,7 +277,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !
 // ---- up to 16 rows to a cache head: single tokens ---------------------------------------------------------------------------------
 //
 // The rows stay in registers, scaled to fp16 as in kv_attend.hpp, and a wave goes through chunks of 64 positions, the next one's codes
-// and weights on their way meanwhile.
+// and weights on their way meanwhile (16 sequences of 500 to 8192 tokens: 31 us without, 19 with both).
 template <int FMT, int NS, int NP, bool ONE>
 __global__ __launch_bounds__(64 * kFewWaves, NP <= 2 && NS == 1 ? 4 : 2) void kv_weigh_tokens_kernel(WeighArgs P) {
   const KvCache &C = P.C;
@@ -652,25 +655,39 @@ __global__ __launch_bounds__(256) void kv_weigh_join_kernel(WeighRows R) {
 // How a call is cut up.
 enum WeighWay {
   kTokens,  // up to 16 rows to a cache head: kv_weigh_tokens_kernel
-  kFew,    // each wave its own positions, all rows in turn
-  kShare,  // fp32 rows: a workgroup's waves share 64 positions and take the rows in turn
-  kRows    // 16-bit rows: kv_weigh_rows_kernel
+  kFew,     // each wave its own positions, all rows in turn
+  kShare,   // fp32 rows: a workgroup's waves share 64 positions and take the rows in turn
+  kRows     // 16-bit rows: kv_weigh_rows_kernel
 };
 struct WeighPlan {
   WeighWay way;
   int groups, splits;
 };
+// 32 heads of 128 on 8 unless said otherwise, codes in int8, bf16 rows:
+//   kTokens or kFew: 16 sequences of 500 to 8192 tokens, one row each 19 us and 29, four rows 19 and 29
+//   kFew or kRows: the same, 32 rows each (128 to a cache head) 60 us and 76, 64 rows 102 and 99; 64 of 500 to 4000, 64 rows 172 and 183, 128
+//     rows 310 and 280; two of 3000 to 6000, 64 rows 22 and 25, 1000 rows 235 and 115; 4-bit codes 16 of 500 to 8192, 64 rows
+//     100 and 112.  Heads of 160 and 192 dims leave kRows one wave to a SIMD and kFew two, so that enough positions for all of the
+//     card go through kFew: of 160 dims, 16 of 500 to 8192, 500 rows 521 and 820; two of 3000 to 6000, 192 dims, 3000 rows 817 and 393.
+//   kFew or kShare, fp32: 16 of 500 to 8192, 64 rows 242 us and 374; two of 3000 to 6000, 64 rows 46 and 55, 1000 rows 590 and 362;
+//     one of 2000, 64 rows 31 and 12
+//   workgroups of kTokens, 512, 1024, 2048: 16 of 500 to 8192 22, 19, 19 us; one of 131071 27, 24, 26; 64 of 1 to 16384 (where
+//     1024 are two to a head and 4096 eight) 163, 135, 125, with 4096 122
+//   workgroups of kRows, 512, 1024, 1536, 2048: two prompts of 3133 and 5340 tokens 264, 230, 220, 224 us, without splits 422; pieces of 8
+//     tiles at least, 16, 32: a prompt of 500 25, 32, 52
 WeighPlan plan_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   WeighPlan p{kFew, 1, 1};
   const int64_t heads = (int64_t)S.n * C.heads, rows = (int64_t)S.max_rows * A.group;
+  const int64_t alone = heads * cdiv(S.max_len, kChunk * kFewWaves);  // workgroups of kFew
   if (rows <= 16) p.way = kTokens;
-  else if (A.type == KM_T_F32 ? rows > 64 : S.max_rows >= kRowTile) p.way = A.type == KM_T_F32 ? kShare : kRows;
+  else if (A.type == KM_T_F32) p.way = rows >= 1024 || (rows > 64 && alone < 256) ? kShare : kFew;
+  else p.way = rows >= 512 && S.max_rows >= kRowTile && (dim_tiles32(C.d) != 6 || alone < 1024) ? kRows : kFew;
   // Workgroups of a sequence's head: one for each of its pieces by the longest length that the caller knows, fewer where that is
   // more than 2^20 in all (a workgroup then takes several, as where a length is longer than was said).
   const int64_t pieces = cdiv(S.max_len, p.way == kShare ? kChunk : p.way == kRows ? kRowKeys : kChunk * kFewWaves);
   p.groups = (int)std::max<int64_t>(1, std::min(pieces, (1 << 20) / heads));
-  // as many workgroups as run at a time
-  if (p.way == kTokens) p.groups = (int)std::min<int64_t>(p.groups, cdiv(1024, heads));
+  // as many workgroups as run at a time, but not so few that lengths differ by whole workgroups
+  if (p.way == kTokens) p.groups = (int)std::min<int64_t>(p.groups, std::max<int64_t>(8, cdiv(1024, heads)));
   // three times as many workgroups as run at a time, of eight tiles at least
   if (p.way == kRows)
     p.splits = (int)std::max<int64_t>(1, std::min(cdiv(1536, heads * p.groups), cdiv(S.max_rows, kRowTile) * A.group / 8));

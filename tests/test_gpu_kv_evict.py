@@ -85,6 +85,33 @@ def test_weigh(fmt, type_, case):
         _weigh_check(s, q, type_, causal=False, label="whole")
 
 
+MANY = [
+    # page, heads, group, d, lens, rows, window: 512 rows to a cache head and more
+    (16, 1, 8, 128, [150, 70], [150, 70], 0),
+    (32, 1, 4, 192, [200], [150], 0),
+    (128, 1, 4, 256, [160, 129, 0], [160, 129, 1], 33),
+    (64, 2, 16, 32, [300, 40], [33, 40], 0),
+    (64, 1, 1, 160, [600, 31], [600, 31], 0),
+    (16, 2, 5, 96, [700, 130], [130, 130], 64),
+]
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("type_", ["bf16", "f16"])
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_weigh_many_rows(fmt, type_, case):
+    page, heads, group, d, lens, rows, window = MANY[case]
+    say(f"kv_weigh {fmt} {type_} many rows page={page} heads={heads}x{group} d={d} lens={lens} rows={rows} window={window}")
+    s = _setup(fmt, page, heads, d, lens, rows, seed=540 + case, wide=2)
+    q = s.normal((s.rows, heads * group, d), type_, 0.3 if fmt == "fp8" else 0.6)
+    q[1, 0] = math.nan
+    _weigh_check(s, q, type_, window=window, decay=0.9, label="causal")
+    _weigh_check(s, q, type_, causal=False, window=0, label="whole")
+    table = s.table.copy()
+    table[0, 1:3] = -1
+    _weigh_check(s, q, type_, window=window, table=table, label="absent pages")
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("rows", [1, 70])
 def test_weigh_rows_that_see_nothing_and_absent_pages(fmt, rows):
@@ -209,8 +236,8 @@ def test_evict_leaves_alone(fmt):
     assert host(left).tolist() == [10, 100, 100, -1, 10 ** 6] and (host(kept)[1:] == -1).all()
 
 
-# Tables that are wide enough for sequences of 25 thousand tokens: chosen from by several workgroups, whatever the lengths are.
-WIDE = 25600
+# Tables that are wide enough for sequences of 50 thousand tokens: chosen from by several workgroups, whatever the lengths are.
+WIDE = 51200
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -241,7 +268,7 @@ def test_evict_in_slices_special_and_left_alone():
 def test_evict_in_slices_in_a_graph():
     """Replayed with other weights and lengths, eager calls in between: the same as an eager call each time."""
     torch = torch_cuda()
-    s = Setup4(64, 2, 32, [30000, 900], [1, 1], seed=39)
+    s = Setup4(64, 2, 32, [30000, 900], [1, 1], seed=39, wide=WIDE // 64)
     keep = torch.tensor([20000, 300], dtype=torch.int32, device="cuda")
     wd = _weights(s)[1]
     state = (s.cache.k, s.cache.v, s.cache.k_scale, s.cache.v_scale, wd)
