@@ -9,9 +9,9 @@
 // all stay where they are is left out of both.
 //
 // Measured: 8 sequences of 4100 tokens, 8 heads of 128 in int8, half of them kept: 12 us to choose (latency: three passes of dependent
-// loads and counts), 35 to gather (values a byte at a time from 64-byte rows, and quotients for codes whose page had another scale: the
-// vector unit is busy half of the time), 12 to scatter (34 MB each way, 5.8 TB/s).  One sequence of 100001 tokens, 4-bit codes, 8192
-// kept: six kernels of 5 to 8 us to choose, each of them mostly its launch and a chain of three dependent loads, 15 to gather, 5 to scatter.
+// loads and counts), 35 to gather (a chain of loads to each token's page, values a byte at a time, quotients for codes whose page had another
+// scale), 12 to scatter (34 MB each way, 5.8 TB/s).  One sequence of 100001 tokens, 4-bit codes, 8192 kept: six kernels of 5 to 8 us to
+// choose, each of them mostly its launch and a chain of three dependent loads, 17 to gather, 5 to scatter.
 #include "kv_pages.hpp"
 
 namespace kmq {
