@@ -10,7 +10,8 @@ import numpy as np
 import pytest
 
 from gpu_util import host, say, torch_cuda
-from test_gpu_kv import DT, _attend_check
+from test_gpu_kv import DT, EIGHT, _attend_check
+from test_gpu_kv import SPLITS as SPLITS8
 
 pytestmark = pytest.mark.gpu
 
@@ -323,6 +324,21 @@ def test_attend_split(name, type_):
     s = Setup4(page, heads, d, lens, rows, seed=41)
     q = s.normal((s.rows, heads * group, d), type_, 0.8)
     _attend_check(s, q, type_, label=name)
+
+
+# The calls of the 8-bit formats that are split up in one way or another, or take workgroups of eight waves.
+CUTS = {n: c for n, c in list(SPLITS8.items()) + [("eight_" + n, c) for n, c in EIGHT.items()] if c[3] % 32 == 0}
+
+
+@pytest.mark.parametrize("type_", ["bf16", "f16"])
+@pytest.mark.parametrize("name", list(CUTS))
+def test_attend_cut_up(name, type_):
+    page, heads, group, d, lens, rows, window, wide = CUTS[name]
+    say(f"kv_attend int4 cut up {name} {type_}")
+    s = Setup4(page, heads, d, lens, rows, seed=700 + list(CUTS).index(name), wide=wide)
+    # fp16 results below its normal range are rounded to steps of 2^-24
+    _attend_check(s, s.normal((s.rows, heads * group, d), type_, 0.4), type_, window=window, label=name,
+                  least=2.0 ** -25 if type_ == "f16" else 0.0)
 
 
 def test_calls_on_a_stream_and_in_a_graph():
