@@ -8,7 +8,8 @@
 // A wave takes 64 positions, whose codes it widens once and keeps in registers as the first operand (as in kv_attend.hpp, lane group
 // g = lane / 16 ends with the scores of positions 16 g .. 16 g + 15 of its row), and goes through the rows 16 at a time.  Codes of all
 // formats are exact in fp16 and in bf16, so 16-bit queries are the second operand as they are; fp32 ones take two halves of fp16
-// after a power of two for each row.  The sums of a row's lane are added up over the sixteen lanes at the end.
+// after a power of two for each row.  bf16 queries reach 2^128, and their products with codes would leave fp32's range: such codes are
+// taken times 2^-40 (weigh_down).  The sums of a row's lane are added up over the sixteen lanes at the end.
 //
 // Four ways (plan_weigh).  Single tokens: kv_weigh_tokens_kernel, bound by the bytes of the keys, 19 us for 78 MB of 16 sequences of
 // 500 to 8192 tokens in int8 (13 at the rate of a read; the longest sequence's workgroups are the last).  A few hundred rows:
@@ -37,6 +38,33 @@ struct WeighArgs {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+// bf16 rows: a position's codes are taken times 2^-40, which is exact, or times 1.  f: the softmax's scale in base 2, ks: the position's.
+// |<q, code>| is at most 2^128 448 256 < 2^145.  Where f ks < 1 the sums then stay below 2^105, what products lose below the least normal
+// number is at most 2^-126 256 2^40 = 2^-78 of a score, and a factor that is raised to that number leaves less than 2^-21 of one.  Elsewhere a sum past
+// 2^128 is a score past 2^128, and the row has no finite log-sum-exp.  4-bit codes: ks lies within [2^-30, 2^30], so f alone decides (f ks < 2^60:
+// the loss is below 2^-18).
+template <int FMT, int TYPE>
+__device__ __forceinline__ float weigh_down(float f, float ks) {
+  if constexpr (TYPE != KM_T_BF16) return 1.0f;
+  return (FMT == KM_KV_I4 ? f < 0x1p30f : f * ks < 1.0f) ? 0x1p-40f : 1.0f;
+}
+// A factor of scores, not 0 and not infinite: -infinity (not seen) and 0 stay what they are.
+__device__ __forceinline__ float weigh_bound(float x) { return fminf(fmaxf(x, 0x1p-126f), 0x1.fffffep127f); }
+// What the products of 16-bit rows are multiplied by.
+template <int FMT, int TYPE>
+__device__ __forceinline__ float weigh_factor(float f, float ks) {
+  const float up = 1.0f / weigh_down<FMT, TYPE>(f, ks);
+  return weigh_bound(FMT == KM_KV_I4 || ks < 1.0f ? f * (ks * up) : (f * up) * ks);
+}
+// Codes as operands beside bf16 rows.
+__device__ __forceinline__ f16x8 weigh_bf16(f16x8 x, float down) {
+  typedef float f32x8 __attribute__((ext_vector_type(8)));
+  f32x8 y;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = fmaf((float)x[i], down, 0.0f);  // widened and multiplied in one instruction
+  return __builtin_bit_cast(f16x8, __builtin_convertvector(y, bf16x8));
+}
+
 // The sum over a lane's row of sixteen, in every lane.
 __device__ __forceinline__ float sum_row(float x) {
 #define KV_ROR(n) x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x120 + n, 0xf, 0xf, false))
@@ -48,10 +76,16 @@ __device__ __forceinline__ float sum_row(float x) {
   return x;
 }
 
+// Waves to a SIMD that the registers have to leave room for.  fp32 rows of up to 128 dims: with room for three, 26 to 37 registers were spilled,
+// 16 sequences of 500 to 8192 with 64 rows each 243 us in int8 and 300 in 4 bits, with two 168 and 165.
+template <int TYPE, int NP, bool MANY>
+constexpr int weigh_waves() {
+  return MANY || TYPE == KM_T_F32 ? (NP <= 3 ? 2 : 1) : NP == 1 ? 4 : NP == 2 ? 3 : NP == 3 ? 2 : 1;
+}
+
 // TYPE: bf16 and fp16 rows as they are, fp32 rows in two halves (NS = 2)
 template <int FMT, int TYPE, int NP, bool MANY, bool ONE>
-__global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !MANY ? 3 : NP <= 3 ? 2 : 1)) void kv_weigh_kernel(
-    WeighArgs P) {
+__global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (weigh_waves<TYPE, NP, MANY>())) void kv_weigh_kernel(WeighArgs P) {
   constexpr int NS = TYPE == KM_T_F32 ? 2 : 1, W = MANY ? kManyWaves : kFewWaves;
   __shared__ float sh[MANY ? W : 1][kChunk];
   const KvCache &C = P.C;
@@ -87,9 +121,13 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !
   const int64_t at = head_at(pv) * C.page + (jm & pmask);
   const float old = mine && P.decay != 0.0f && jm < q.len - q.n ? P.weight[at] : 0.0f;
 
+  const float f = A.scale * kLog2e;
   // keys; dims past d are 0
   f16x8 kf[4][NP][2];
   {
+    float down = FMT == KM_KV_I4 || TYPE != KM_T_BF16 ? 1.0f : C.ks[head_at(pk)];
+    down = weigh_down<FMT, TYPE>(f, down);
+    asm("" : "+v"(down));  // no second copy of all that follows
     const uint8_t *kp = C.k + head_at(pk) * hb + ((j0 + (ONE ? 0 : 16 * kr)) & pmask) * db;
     Codes16<FMT> kw[4][NP];
 #pragma unroll
@@ -111,22 +149,18 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !
             const f16x8 y = kf[st][p][k];
             kf[st][p][k] = f16x8{y[0], y[2], y[4], y[6], y[1], y[3], y[5], y[7]};
           }
-          if constexpr (TYPE == KM_T_BF16) {
-            typedef float f32x8 __attribute__((ext_vector_type(8)));
-            kf[st][p][k] = __builtin_bit_cast(f16x8, __builtin_convertvector(__builtin_convertvector(kf[st][p][k], f32x8), bf16x8));
-          }
+          if constexpr (TYPE == KM_T_BF16) kf[st][p][k] = weigh_bf16(kf[st][p][k], down);
         }
   }
-  // what a score is multiplied by, for each of the lane's 16 positions; not 0, so that -infinity stays
+  // what a score is multiplied by, for each of the lane's 16 positions; fp32 rows: the position's scale alone
   float ck[16];
   {
-    const float f = A.scale * kLog2e;
     if constexpr (FMT == KM_KV_I4) {
       const float ks = mine ? C.ks[at] : 1.0f;
-      each<16>([&](auto e) { ck[e] = fmaxf(f * kv_row_bcast<e>(ks), 0x1p-126f); });
+      each<16>([&](auto e) { ck[e] = NS == 2 ? kv_row_bcast<e>(ks) : weigh_factor<FMT, TYPE>(f, kv_row_bcast<e>(ks)); });
     } else {
       const float ks = j0 + 16 * g < q.len && there ? C.ks[head_at(pv)] : 1.0f;
-      ck[0] = fmaxf(f * ks, 0x1p-126f);
+      ck[0] = NS == 2 ? ks : weigh_factor<FMT, TYPE>(f, ks);
 #pragma unroll
       for (int e = 1; e < 16; ++e) ck[e] = ck[0];
     }
@@ -185,7 +219,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !
     const bool counts = fabsf(lse) < INFINITY;
     const float nl = counts ? -lse * kLog2e : -INFINITY;
     f16x8 qf[NP][2][NS];
-    float c32 = 1.0f;
+    float c32 = 1.0f;  // fp32 rows: what a score is multiplied by, 4-bit codes without the position's scale
     if (!__all(counts)) {  // rows that do not count may hold NaN
 #pragma unroll
       for (int p = 0; p < NP; ++p)
@@ -206,7 +240,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !
         for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(v[p][i]));
       }
       float f;
-      q_scale(max_groups(top), 1.0f / kLog2e, &f, &c32);
+      q_scale(max_groups(top), A.scale, &f, &c32);
+      c32 = weigh_bound(FMT == KM_KV_I4 ? c32 : c32 * ck[0]);
 #pragma unroll
       for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -238,9 +273,9 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !
             else
               s[st] = mfma16(kf[st][p][k], qf[p][k][z], s[st]);
           }
-    if constexpr (NS == 2) {
+    if constexpr (NS == 2 && FMT == KM_KV_I4) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e / 4][e % 4] *= c32;
+      for (int e = 0; e < 16; ++e) s[e / 4][e % 4] *= ck[e];
     }
     if (!__all(j0 >= see0 && j0 + kChunk <= see1)) {
       int jg = j0 + 16 * g;
@@ -252,7 +287,7 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (NP <= 2 && !
       }
     }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) sum[e] += __builtin_amdgcn_exp2f(fmaf(s[e / 4][e % 4], ck[e], nl));
+    for (int e = 0; e < 16; ++e) sum[e] += __builtin_amdgcn_exp2f(fmaf(s[e / 4][e % 4], NS == 2 ? c32 : ck[e], nl));
   }
 
   float total = 0.0f;
@@ -481,13 +516,15 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
     const bool mine = j0 < q.len;
     // keys: row m of operand tt is position 32 tt + m
     f16x8 kf[2][KS];
-    float ck[FMT == KM_KV_I4 ? 32 : 4];  // what a score is multiplied by; not 0, so that -infinity stays
+    float ck[FMT == KM_KV_I4 ? 32 : 4];  // what a score is multiplied by
     if (mine) {
       const float f = A.scale * kLog2e;
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         const int j = j0 + 32 * tt + m, pg = page_of(ONE ? j0 : j);
         const uint8_t *kp = C.k + head_at(pg) * hb + (j & pmask) * db;
+        float down = FMT == KM_KV_I4 || TYPE != KM_T_BF16 ? 1.0f : C.ks[head_at(pg)];
+        down = weigh_down<FMT, TYPE>(f, down);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           const uint8_t *from = kp + (int)kv_bytes<FMT>(min(16 * k + 8 * g, d - 8));
@@ -500,10 +537,7 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
             y = kv_widen8<FMT>(w.x, w.y);
           }
           if (16 * k + 8 * g >= d) y = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
-          if constexpr (TYPE == KM_T_BF16) {
-            typedef float f32x8 __attribute__((ext_vector_type(8)));
-            y = __builtin_bit_cast(f16x8, __builtin_convertvector(__builtin_convertvector(y, f32x8), bf16x8));
-          }
+          if constexpr (TYPE == KM_T_BF16) y = weigh_bf16(y, down);
           kf[tt][k] = y;
         }
       }
@@ -513,13 +547,13 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
           const int j = j0 + 8 * y + 4 * g, pg = page_of(ONE ? j0 : j);
           const f32x4 ks = *reinterpret_cast<const f32x4 *>(C.ks + head_at(pg) * C.page + (j & pmask));
 #pragma unroll
-          for (int z = 0; z < 4; ++z) ck[4 * y + z] = there_at(pg) && j + z < q.len ? fmaxf(f * ks[z], 0x1p-126f) : 1.0f;
+          for (int z = 0; z < 4; ++z) ck[4 * y + z] = there_at(pg) && j + z < q.len ? weigh_factor<FMT, TYPE>(f, ks[z]) : 1.0f;
         }
       } else {
 #pragma unroll
         for (int y = 0; y < 4; ++y) {  // runs of 16
           const int j = j0 + 16 * y, pg = page_of(ONE ? j0 : j);
-          ck[y] = there_at(pg) && j < q.len ? fmaxf(f * C.ks[head_at(pg)], 0x1p-126f) : 1.0f;
+          ck[y] = there_at(pg) && j < q.len ? weigh_factor<FMT, TYPE>(f, C.ks[head_at(pg)]) : 1.0f;
         }
       }
     }
