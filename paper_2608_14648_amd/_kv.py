@@ -148,10 +148,12 @@ def _rows_of(t: torch.Tensor, name: str, seqs: KvSeqs, heads: int, d: int, dtype
                          "detach it")
     if t.shape != (seqs.rows, heads, d):
         raise ValueError(f"{name} must be [{seqs.rows}, {heads}, {d}] (got {tuple(t.shape)})")
+    if seqs.rows == 0:  # strides of nothing are of no meaning
+        return KmKvRows(t.data_ptr(), 0, 0)
     row, head, one = t.stride()
     if one != 1:
         raise ValueError(f"{name}'s last axis must be contiguous")
-    if seqs.rows <= 1:  # the stride of an axis of one is of no meaning
+    if seqs.rows == 1:  # the stride of an axis of one is of no meaning
         row = 0
     if heads == 1:
         head = 0
