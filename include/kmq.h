@@ -546,7 +546,8 @@ km_status kv_rotate(const km_kv_rotary *rotary, const km_kv_seqs *seqs, const in
  * kv_weigh -- the attention weight that cached tokens get from the rows' queries, added to what they had:
  *   weight[page][head][token] of every position j of the sequences = decay * what it was + sum over the rows and their query heads
  *   of that cache head of exp(scale <q, k_j> - lse), over the rows that see j (as in kv_attend).  The call's own positions (the
- *   last ones, one for each row) begin with the sum alone, and with decay = 0 nothing that was there is looked at.
+ *   last ones, one for each row) begin with the sum alone, and with decay = 0 nothing that was there is looked at.  A sequence without
+ *   rows in the call has no sum: decay * what it was, with decay = 0 0.  A call without any rows needs neither q nor lse.
  *   lse: float[rows][q_heads] as kv_attend leaves it for these rows and this cache; a row's head whose lse is not finite adds nothing.
  *   weight: DEVICE float[pages][heads][page].  decay: finite, >= 0.  Sums are fp32, in an order that does not depend on scheduling.
  *   Positions on pages that are not there have no weight.  No two sequences of a call may have a page in common.

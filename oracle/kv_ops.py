@@ -126,7 +126,7 @@ def weigh(cache, table, lens, starts, q, lse, weight, scale, causal=True, window
     out = np.array(weight, np.float64)
     big, els = np.zeros_like(out), np.zeros_like(out)
     for b, ln, r0, n in cache._seqs(table, lens, starts):
-        if n == 0 or ln == 0:
+        if ln == 0:
             continue
         k, _ = cache.rows(table[b], 0, ln)
         j = np.arange(ln)

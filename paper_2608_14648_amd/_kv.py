@@ -381,7 +381,8 @@ def kv_weigh(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, lse: torch.Tensor, w
     head, to `weight` (float32 [pages, heads, page], in place) times decay.
 
     q, scale, causal and window are those of the kv_attend call that left lse (its log-sum-exp, float32 [rows, q_heads]).  The call's own
-    tokens begin with this sum; with decay = 0 all tokens do.  Rows whose lse is not finite add nothing.  No two sequences of a call
+    tokens begin with this sum; with decay = 0 all tokens do.  Rows whose lse is not finite add nothing.  Sequences without rows in the
+    call age like the others: their weights are multiplied by decay, with decay = 0 cleared.  No two sequences of a call
     may have a page in common."""
     _same(cache, seqs)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
@@ -393,8 +394,6 @@ def kv_weigh(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, lse: torch.Tensor, w
     if tuple(lse.shape) != (seqs.rows, q_heads):
         raise ValueError(f"lse must be [{seqs.rows}, {q_heads}] (got {tuple(lse.shape)})")
     _weights(weight, cache)
-    if seqs.rows == 0:
-        return
     lb = lib()
     flags, window, t = KM_KV_CAUSAL if causal else 0, _i32(window), _TYPES[q.dtype]
     need = lb.kv_weigh_bytes(cache._ref, seqs._ref, q_heads, flags, window, t)

@@ -1173,7 +1173,7 @@ static km_status check_cache(const km_kv_cache *c, KvCache *o) {
   return KM_OK;
 }
 
-// OK with o->n == 0: a call without rows, or with whole sequences (their rows are not looked at) one without sequences
+// OK with o->n == 0: a call without rows, or with whole sequences (whether they have rows is not looked at) one without sequences
 static km_status check_seqs(const km_kv_seqs *s, const KvCache &c, KvSeqs *o, bool whole = false) {
   KMQ_CHECK(s != nullptr, KM_EINVAL, "sequences descriptor is NULL");
   KMQ_CHECK(s->n >= 0 && s->rows >= 0 && s->max_rows >= 0 && s->max_len >= 0, KM_EINVAL,
@@ -1367,12 +1367,16 @@ km_status kv_rotate(const km_kv_rotary *rotary, const km_kv_seqs *seqs, const in
   return launch_kv_rotate(r, type, reinterpret_cast<hipStream_t>(stream));
 }
 
+static bool weigh_rows(const KvSeqs &s) { return s.rows > 0 && s.max_rows > 0; }
+
 static km_status check_weigh(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t q_heads, int32_t flags, int32_t window,
                              int32_t type, KvCache *c, KvSeqs *s, KvAttend *a) {
   km_status st = check_cache(cache, c);
-  if (st == KM_OK) st = check_seqs(seqs, *c, s);
+  if (st == KM_OK) st = check_seqs(seqs, *c, s, true);  // sequences without rows age too
   if (st == KM_OK) st = check_queries(*c, *s, q_heads, flags, window, type, a);
   if (st != KM_OK) return st;
+  KMQ_CHECK(s->n == 0 || s->starts != nullptr || !weigh_rows(*s) || s->rows == (int64_t)s->n * s->max_rows, KM_EINVAL,
+            "without starts rows must be n * max_rows");
   KMQ_CHECK(s->n < 2 || s->table_ld != 0, KM_EINVAL, "sequences of one table row share their pages' weights");
   KMQ_CHECK((int64_t)s->n * c->heads <= (1 << 20), KM_EINVAL, "n * heads = %lld must be <= 2^20", (long long)s->n * c->heads);
   return s->n ? check_grid(kv_weigh_blocks(*c, *s, *a)) : KM_OK;
@@ -1401,9 +1405,14 @@ km_status kv_weigh(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv
   KMQ_CHECK(scale > 0.0f && std::isfinite(scale), KM_EINVAL, "scale = %g must be finite and > 0", (double)scale);
   KMQ_CHECK(decay >= 0.0f && std::isfinite(decay), KM_EINVAL, "decay = %g must be finite and >= 0", (double)decay);
   if (s.n == 0) return KM_OK;
-  KMQ_CHECK(lse != nullptr && weight != nullptr, KM_EINVAL, "NULL argument");
-  st = check_rows(q, type, "q", &a.q);
-  if (st != KM_OK) return st;
+  KMQ_CHECK(weight != nullptr, KM_EINVAL, "NULL argument");
+  if (weigh_rows(s)) {
+    KMQ_CHECK(lse != nullptr, KM_EINVAL, "NULL argument");
+    st = check_rows(q, type, "q", &a.q);
+    if (st != KM_OK) return st;
+  } else if (decay == 1.0f) {
+    return KM_OK;
+  }
   a.scale = scale;
   a.lse = const_cast<float *>(lse);  // read only
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);

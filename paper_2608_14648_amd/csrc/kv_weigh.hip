@@ -83,6 +83,18 @@ constexpr int weigh_waves() {
   return MANY || TYPE == KM_T_F32 ? (NP <= 3 ? 2 : 1) : NP == 1 ? 4 : NP == 2 ? 3 : NP == 3 ? 2 : 1;
 }
 
+// A sequence without rows in the call: its weights times decay, by the workgroups of its heads.
+__device__ __forceinline__ void weigh_idle(const WeighArgs &P, const KvSeq &q, int b, int h, int group) {
+  if (P.decay == 1.0f) return;
+  const KvCache &C = P.C;
+  for (int64_t j = (int64_t)group * blockDim.x + threadIdx.x; j < q.len; j += (int64_t)P.groups * blockDim.x) {
+    const int64_t pg = P.S.table[(int64_t)b * P.S.table_ld + (j >> C.shift)];
+    if (pg < 0 || pg >= C.pages) continue;
+    float *w = P.weight + (pg * C.heads + h) * C.page + (j & (C.page - 1));
+    *w = P.decay != 0.0f ? *w * P.decay : 0.0f;
+  }
+}
+
 // TYPE: bf16 and fp16 rows as they are, fp32 rows in two halves (NS = 2)
 template <int FMT, int TYPE, int NP, bool MANY, bool ONE>
 __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (weigh_waves<TYPE, NP, MANY>())) void kv_weigh_kernel(WeighArgs P) {
@@ -97,7 +109,8 @@ __global__ __launch_bounds__(64 * (MANY ? kManyWaves : kFewWaves), (weigh_waves<
   const int b = (int)(x % (uint32_t)P.S.n), group = (int)(x / (uint32_t)P.S.n);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   KvSeq q;
-  if (!kv_seq(P.S, C.page, b, &q) || q.n == 0) return;
+  if (!kv_seq(P.S, C.page, b, &q)) return;
+  if (q.n == 0) return weigh_idle(P, q, b, h, group);
   const int d = C.d, rows = q.n * A.group;
   const KvNibbles nib = kv_nibbles();
   const int64_t hb = kv_bytes<FMT>((int64_t)C.page * d);
@@ -323,7 +336,8 @@ __global__ __launch_bounds__(64 * kFewWaves, NP <= 2 && NS == 1 ? 4 : 2) void kv
   const int group = (int)(x % (uint32_t)P.groups), b = (int)(x / (uint32_t)P.groups);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   KvSeq q;
-  if (!kv_seq(P.S, C.page, b, &q) || q.n == 0) return;
+  if (!kv_seq(P.S, C.page, b, &q)) return;
+  if (q.n == 0) return weigh_idle(P, q, b, h, group);
   const int d = C.d, rows = q.n * A.group, chunks = (int)cdiv(q.len, kChunk), step = P.groups * kFewWaves;
   const KvNibbles nib = kv_nibbles();
   const int64_t hb = kv_bytes<FMT>((int64_t)C.page * d);
@@ -487,7 +501,9 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
   x /= (uint32_t)R.splits;
   const int b = (int)(x % (uint32_t)P.S.n), group0 = (int)(x / (uint32_t)P.S.n);
   KvSeq q;
-  if (!kv_seq(P.S, C.page, b, &q) || q.n == 0) return;
+  if (!kv_seq(P.S, C.page, b, &q)) return;
+  if (q.n == 0 && split == 0) weigh_idle(P, q, b, h, group0);
+  if (q.n == 0) return;
   const bool parts = weigh_split(R, q);
   if (!parts && split > 0) return;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), m = lane & 31, g = lane >> 5;

@@ -83,3 +83,78 @@ def test_queries_of_zero_over_the_largest_keys(fmt, type_, way):
     s.orc.mul[0][:] = np.float32(2.0 ** -119)
     q = s.torch.zeros((s.rows, heads * group, d), dtype=s.normal((1,), type_).dtype, device="cuda")
     _check(s, q, type_, 4096.0, "zero")
+
+
+# As above with sequences that have no rows in the call (lengths, rows): one idle, one idle and empty, one idle that is longer than the others,
+# one whose length does not fit.
+IDLE = {
+    "tokens": (2, 2, 64, [100, 40, 0, 333, 33], [1, 0, 0, 0, 3]),
+    "few": (1, 4, 64, [130, 40, 0, 333, 90], [5, 0, 0, 0, 9]),
+    "some": (2, 4, 128, [100, 40, 0, 700, 300], [5, 0, 0, 0, 40]),
+    "many": (1, 8, 96, [200, 40, 0, 900, 70], [150, 0, 0, 0, 40]),
+}
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("type_", ["bf16", "f32"])
+@pytest.mark.parametrize("way", list(IDLE))
+def test_sequences_without_rows_age_too(fmt, type_, way):
+    heads, group, d, lens, rows = IDLE[way]
+    say(f"kv_weigh idle sequences {fmt} {type_} {way}")
+    s = _setup(fmt, 32, heads, d, lens, rows, seed=902, wide=2)
+    q = s.normal((s.rows, heads * group, d), type_, 0.3)
+    for decay in (0.9, 1.0, 0.0):
+        _check(s, q, type_, 1 / math.sqrt(d), f"decay {decay}", decay)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("rows", [0, 1, 70])
+def test_what_idle_sequences_leave_alone(fmt, rows):
+    """Only their own positions change, by one rounding: not those behind the end, on pages that are not there or of lengths that do not
+    fit; NaN stays with decay 0.5 and goes with 0.  rows = 0: the whole call has none, and the same holds."""
+    torch = torch_cuda()
+    s = _setup(fmt, 16, 2, 64, [100, 50, 77, 40], [rows, 0, 0, 0], seed=903, wide=1)
+    table, lens = s.table.copy(), [100, 50, 77, 10 ** 6]
+    table[2, 1:3] = (-1, 10 ** 6)
+    seqs = s.seqs_of(lens, s.starts, table)
+    q = s.normal((rows, 8, 64), "bf16")
+    lse = torch.zeros((rows, 8), device="cuda")
+    w, wd = _weights(s)
+    w[s.table[1, 0], 1, 3] = np.nan
+    mine = np.zeros(w.shape, bool)
+    for b in ((1, 2) if rows else (0, 1, 2)):
+        for j in range(lens[b]):
+            if 0 <= table[b, j // 16] < s.cache.pages:
+                mine[table[b, j // 16], :, j % 16] = True
+    first = np.zeros(w.shape, bool)
+    first[s.table[0, :7]] = rows > 0  # of the sequence that has rows
+    for decay in (0.5, 0.9, 1.0, 0.0):
+        wd.copy_(torch.from_numpy(w))
+        s.km.kv_weigh(s.cache, seqs, q, lse, wd, decay=decay)
+        torch.cuda.synchronize()
+        want = np.where(mine, w * np.float32(decay) if decay else np.float32(0), w)
+        np.testing.assert_array_equal(np.where(first, 0, host(wd)), np.where(first, 0, want), err_msg=f"decay {decay}")
+
+
+def test_a_call_without_rows_in_a_graph():
+    """Captured, replayed with other lengths; one sequence and many, without starts."""
+    torch = torch_cuda()
+    s = _setup("int4", 16, 2, 64, [100, 50], [1, 1], seed=904)
+    w, wd = _weights(s)
+    seqs = s.km.KvSeqs(s.seqs.table, s.seqs.lens, rows=0, max_rows=0)
+    q, lse = torch.empty((0, 4, 64), device="cuda"), torch.empty((0, 4), device="cuda")
+    s.km.kv_weigh(s.cache, seqs, q, lse, wd, decay=0.5)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s.km.kv_weigh(s.cache, seqs, q, lse, wd, decay=0.5)
+    for n in (100, 30, 0):
+        wd.copy_(torch.from_numpy(w))
+        s.seqs.lens.copy_(torch.tensor([n, 50], dtype=torch.int32))
+        g.replay()
+        torch.cuda.synchronize()
+        want = w.copy()
+        for b, ln in enumerate((n, 50)):
+            for j in range(ln):
+                want[s.table[b, j // 16], :, j % 16] *= np.float32(0.5)
+        np.testing.assert_array_equal(host(wd), want)
