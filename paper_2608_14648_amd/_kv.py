@@ -350,13 +350,13 @@ def kv_rotate(rotary: KvRotary, at: KvSeqs | torch.Tensor, q: torch.Tensor, k: t
 
 def _check_outputs(q, k, q_out, k_out):
     """Rows that are written overlap none of the others, but may be the ones that they are made of."""
-    for out, own, name in ((q_out, q, "q_out"), (k_out, k, "k_out")):
+    for out, name, own, of_own, other, of_other in ((q_out, "q_out", q, "q", k, "k"), (k_out, "k_out", k, "k", q, "q")):
         if out is None:
             continue
-        for t, of in ((q, "q"), (k, "k")):
-            same = t is own and t is not None and t.data_ptr() == out.data_ptr() and t.stride() == out.stride()
-            if t is not None and not same and not _apart(out, t):
-                raise ValueError(f"{name} overlaps {of} and is not the same rows")
+        if (own.data_ptr(), own.stride()) != (out.data_ptr(), out.stride()) and not _apart(out, own):
+            raise ValueError(f"{name} overlaps {of_own} and is not the same rows")
+        if other is not None and not _apart(out, other):
+            raise ValueError(f"{name} overlaps {of_other}")
     if q_out is not None and k_out is not None and not _apart(q_out, k_out):
         raise ValueError("q_out and k_out overlap")
 

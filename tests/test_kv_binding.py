@@ -30,3 +30,22 @@ def test_strides_of_no_rows_mean_nothing():
         one = km.KvSeqs(t(3, 4, dtype=torch.int32), t(3, dtype=torch.int32))
         with pytest.raises(ValueError, match="contiguous"):
             km.kv_attend(cache, one, torch.empty_strided((3, 2, 64), (256, 128, 2), dtype=torch.bfloat16, device="cuda:0"))
+
+
+@needs_lib
+def test_rows_turned_in_place_are_not_read_for_others():
+    """q_out may be q's own rows, but then k must not be read from them: neither as the same tensor nor as a view, and the other way round."""
+    import paper_2608_14648_amd as km
+    torch = pytest.importorskip("torch")
+    from paper_2608_14648_amd._kv import _check_outputs
+    buf = torch.empty((6, 10, 16))
+    x, y, z = buf[:, :3], buf[:, 3:6], buf[:, 6:9]
+    view = buf[:, :3]
+    # in place, apart, or not given
+    for q, k, q_out, k_out in ((x, y, x, y), (x, y, view, y), (x, None, x, None), (x, y, x, z), (x, y, z, y), (x, x, y, z), (x, x, y, None),
+                               (x, y, None, y)):
+        _check_outputs(q, k, q_out, k_out)
+    for q, k, q_out, k_out in ((x, x, x, None), (x, x, x, y), (x, x, None, x), (x, x, y, x), (x, view, x, y), (view, x, x, y),
+                               (x, view, y, x), (x, x, view, None), (x, x, x, x), (x, y, y, None), (x, y, None, x), (x, y, y, x)):
+        with pytest.raises(ValueError, match="overlap"):
+            _check_outputs(q, k, q_out, k_out)
