@@ -348,12 +348,17 @@ def kv_rotate(rotary: KvRotary, at: KvSeqs | torch.Tensor, q: torch.Tensor, k: t
     return qo_t, ko_t
 
 
+def _same_rows(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether rows a and b, of one shape, lie in the same places (the stride of an axis of one is of no meaning)."""
+    return a.data_ptr() == b.data_ptr() and all(n == 1 or s == z for n, s, z in zip(a.shape, a.stride(), b.stride()))
+
+
 def _check_outputs(q, k, q_out, k_out):
     """Rows that are written overlap none of the others, but may be the ones that they are made of."""
     for out, name, own, of_own, other, of_other in ((q_out, "q_out", q, "q", k, "k"), (k_out, "k_out", k, "k", q, "q")):
         if out is None:
             continue
-        if (own.data_ptr(), own.stride()) != (out.data_ptr(), out.stride()) and not _apart(out, own):
+        if not _same_rows(out, own) and not _apart(out, own):
             raise ValueError(f"{name} overlaps {of_own} and is not the same rows")
         if other is not None and not _apart(out, other):
             raise ValueError(f"{name} overlaps {of_other}")

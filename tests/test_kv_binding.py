@@ -49,3 +49,16 @@ def test_rows_turned_in_place_are_not_read_for_others():
                                (x, view, y, x), (x, x, view, None), (x, x, x, x), (x, y, y, None), (x, y, None, x), (x, y, y, x)):
         with pytest.raises(ValueError, match="overlap"):
             _check_outputs(q, k, q_out, k_out)
+
+
+@needs_lib
+def test_in_place_whatever_the_stride_of_an_axis_of_one():
+    import paper_2608_14648_amd as km  # noqa: F401
+    torch = pytest.importorskip("torch")
+    from paper_2608_14648_amd._kv import _check_outputs
+    buf = torch.empty(1000)
+    for shape, a, b in (((1, 3, 16), (160, 16, 1), (48, 16, 1)), ((5, 1, 16), (160, 16, 1), (160, 160, 1)), ((1, 1, 16), (1, 1, 1), (16, 16, 1))):
+        _check_outputs(buf.as_strided(shape, a), None, buf.as_strided(shape, b), None)
+    for shape, a, b in (((2, 3, 16), (160, 16, 1), (48, 16, 1)), ((5, 2, 16), (160, 16, 1), (160, 80, 1))):
+        with pytest.raises(ValueError, match="same rows"):
+            _check_outputs(buf.as_strided(shape, a), None, buf.as_strided(shape, b), None)
