@@ -119,14 +119,17 @@ __global__ __launch_bounds__(kMoveThreads) void kv_write4_kernel(KvCache C, KvSe
       const u32x2 w = __any(mul == 0x1p-30f) ? codes8<true>(x, mul) : codes8<false>(x, mul);
       if (!in || r >= rows) continue;
       if (c == 0) scale[r] = 1.0f / mul;
-      if (values) *reinterpret_cast<u32x2 *>(turn + (r * ld + c * 8) / 4) = w;
-      else *reinterpret_cast<uint32_t *>(dst + (j.i0 + r) * (d / 2) + c * 4) = halve8(w);
+      if (values) {  // rows of turn are an odd number of dwords apart: two stores, not one of eight bytes
+        turn[(r * ld + c * 8) / 4] = w.x;
+        turn[(r * ld + c * 8) / 4 + 1] = w.y;
+      } else {
+        *reinterpret_cast<uint32_t *>(dst + (j.i0 + r) * (d / 2) + c * 4) = halve8(w);
+      }
     }
   }
   if (!values) return;
   __syncthreads();
   // 16 tokens of four dims at a time, neighbouring threads the tokens of a dim's row
-  const uint8_t *tb = reinterpret_cast<const uint8_t *>(turn);
   const int ng = C.page / 16;
   for (int i = t; i < ng * (d / 4); i += kMoveThreads) {
     int g, c4;
