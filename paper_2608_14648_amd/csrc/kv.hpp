@@ -1,4 +1,4 @@
-// The key/value cache in 8 bits: launch-facing descriptions and the conversions that its kernels share.
+// The key/value cache in 8 and 4 bits: launch-facing descriptions and the conversions that its kernels share.
 #pragma once
 
 #include "common.hpp"
@@ -20,9 +20,9 @@ struct KvCache {
   int heads;
   int d;
   int64_t pages;
-  uint8_t *k;  // [pages][heads][page][d]
-  uint8_t *v;  // [pages][heads][d][page]
-  float *ks;   // [pages][heads]
+  uint8_t *k;  // [pages][heads][page][d]; 4-bit codes: [pages][heads][page][d / 2] bytes
+  uint8_t *v;  // [pages][heads][d][page]; 4-bit codes: [pages][heads][d][page / 2] bytes
+  float *ks;   // [pages][heads]; 4-bit codes: [pages][heads][page]
   float *vs;
 };
 
@@ -88,7 +88,7 @@ __device__ __forceinline__ float kv_mul4_of_top(float top) {
 template <int FMT>
 __host__ __device__ constexpr int64_t kv_bytes(int64_t n) { return FMT == KM_KV_I4 ? n / 2 : n; }
 
-// Four codes of a dword, 8 bits each, as halves: both formats' values are exact in fp16.
+// Four codes of a dword, 8 bits each, as halves: the values of int8 and e4m3 are exact in fp16.
 template <int FMT>
 __device__ __forceinline__ void kv_widen4(uint32_t c, f16x2 *lo, f16x2 *hi) {
   if constexpr (FMT == KM_KV_I8) {

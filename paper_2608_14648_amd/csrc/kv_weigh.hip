@@ -581,44 +581,44 @@ __global__ __launch_bounds__(64 * kRowWaves, ND <= 4 ? 2 : 1) void kv_weigh_rows
     const int64_t tiles = (int64_t)nb * A.group, ns = parts ? R.splits : 1;
     const int z0 = (int)(tiles * split / ns), z1 = (int)(tiles * (split + 1) / ns);
     int lh = nb ? z0 / nb : 0, lb = b0 + z0 - lh * nb;  // head and block of the tile that is loaded next
-    u32x4 raw[1][NI];
-    float lse[1];  // of token t, in the first half of a wave
-    auto load = [&](int to) {
+    u32x4 raw[NI];
+    float lse;  // of token t, in the first half of a wave
+    auto load = [&] {
       const int64_t row = q.row0 + (int64_t)lb * kRowTile;
       const uint16_t *base = static_cast<const uint16_t *>(A.q.p) + row * A.q.row + (int64_t)(h * A.group + lh) * A.q.head;
       const int left = min(q.n - lb * kRowTile, kRowTile);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const bool in = prow[i] < left;
-        raw[to][i] = *reinterpret_cast<const u32x4 *>(base + (in ? q_at[i] : 0));
+        raw[i] = *reinterpret_cast<const u32x4 *>(base + (in ? q_at[i] : 0));
       }
-      if (t < kRowTile) lse[to] = t < left ? A.lse[(row + t) * C.heads * A.group + h * A.group + lh] : INFINITY;
+      if (t < kRowTile) lse = t < left ? A.lse[(row + t) * C.heads * A.group + h * A.group + lh] : INFINITY;
       if (++lb == b1) {
         lb = b0;
         ++lh;
       }
     };
-    auto store = [&](int z, int from) {
+    auto store = [&](int z) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         if (prow[i] >= kRowTile) continue;
-        *reinterpret_cast<u32x4 *>(&qt[z & 1][prow[i] * LD + 16 * (t + i * T - prow[i] * per)]) = raw[from][i];
+        *reinterpret_cast<u32x4 *>(&qt[z & 1][prow[i] * LD + 16 * (t + i * T - prow[i] * per)]) = raw[i];
       }
-      if (t < kRowTile) stat[z & 1][t] = fabsf(lse[from]) < INFINITY ? -lse[from] * kLog2e : -INFINITY;
+      if (t < kRowTile) stat[z & 1][t] = fabsf(lse) < INFINITY ? -lse * kLog2e : -INFINITY;
     };
     float sum[32];
 #pragma unroll
     for (int e = 0; e < 32; ++e) sum[e] = 0.0f;
     int cb = lb;  // block of the tile at hand
     if (z0 < z1) {
-      load(0);
-      store(z0, 0);
-      if (z0 + 1 < z1) load(0);
+      load();
+      store(z0);
+      if (z0 + 1 < z1) load();
       __syncthreads();
     }
     for (int z = z0; z < z1; ++z) {
-      if (z + 1 < z1) store(z + 1, 0);
-      if (z + 2 < z1) load(0);
+      if (z + 1 < z1) store(z + 1);
+      if (z + 2 < z1) load();
       const int pos0 = first + cb * kRowTile;  // position of the tile's first token
       if (mine && (!A.causal || pos0 + kRowTile > j0) && (!A.window || (int64_t)pos0 < (int64_t)j0 + kChunk - 1 + A.window)) {
         f32x16v s[2];
