@@ -550,7 +550,8 @@ km_status kv_rotate(const km_kv_rotary *rotary, const km_kv_seqs *seqs, const in
  *   rows in the call has no sum: decay * what it was, with decay = 0 0.  A call without any rows needs neither q nor lse.
  *   lse: float[rows][q_heads] as kv_attend leaves it for these rows and this cache; a row's head whose lse is not finite adds nothing.
  *   weight: DEVICE float[pages][heads][page].  decay: finite, >= 0.  Sums are fp32, in an order that does not depend on scheduling.
- *   Positions on pages that are not there have no weight.  No two sequences of a call may have a page in common.
+ *   Positions on pages that are not there have no weight.  No two sequences of a call may have a page in common, and none may have one
+ *   twice (within its length): the sums of positions that share a weight would overwrite each other.
  *   q_heads, scale, flags, window, type: as in kv_attend; max_rows * q_heads / heads < 2^30.
  *   ws (nullable): kv_weigh_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the pool.
  */
@@ -565,10 +566,10 @@ int64_t kv_weigh_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t
 /*
  * kv_evict -- every sequence keeps keep[b] of its tokens, each head its own, and closes the gaps: the first `first` and the last
  *   `recent` positions, then those of the largest weight, ties to the lower position (first and recent count as of infinite
- *   weight, NaN as less than all).  The kept tokens of a head, in their order,
- *   become its positions 0, 1, ...: codes, scales and weights move; what lies behind them stays as it is.  8-bit codes take the
- *   smallest multiplier of the tokens that come to their page and are coded again where theirs was larger, as in kv_write; 4-bit
- *   ones do not change.  The pages behind the last kept position are free then.
+ *   weight, NaN as less than all; where keep[b] < first + recent, the lower positions of those two stay, so the most recent go).  The
+ *   kept tokens of a head, in their order, become its positions 0, 1, ...: codes, scales and weights move; what lies behind
+ *   them stays as it is.  8-bit codes take the smallest multiplier of the tokens that come to their page and are coded again
+ *   where theirs was larger, as in kv_write; 4-bit ones do not change.  The pages behind the last kept position are free then.
  *   seqs: n, max_pages, table, table_ld and lens are looked at; a sequence whose length does not fit, or that has a page that is
  *   not there, is left as it is.
  *   weight: DEVICE float[pages][heads][page].  keep: DEVICE int32[n], of which max(0, min(keep[b], max_keep)) counts.
@@ -576,13 +577,14 @@ int64_t kv_weigh_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t
  *   kept: DEVICE int32[n][heads][max_keep], the position that each kept token had, -1 where there is none.  lens (out): DEVICE
  *   int32[n], how many are kept (of a sequence that is left as it is: its length); not seqs->lens.
  *   ws (nullable): kv_evict_bytes of device memory, 16-byte aligned, used until the call's work is done; NULL: taken from the pool.
- *   No two sequences of a call may have a page in common.
+ *   No two sequences of a call may have a page in common, and none may have one twice (within its length).
  */
 km_status kv_evict(const km_kv_cache *cache, const km_kv_seqs *seqs, float *weight, const int32_t *keep, int32_t max_keep,
                    int32_t first, int32_t recent, int32_t *kept, int32_t *lens, void *ws, int64_t ws_bytes,
                    km_stream stream);
 
-/* Bytes of ws that kv_evict uses for these arguments (< 0: a km_status). */
+/* Bytes of ws that kv_evict uses for these arguments (< 0: a km_status): mostly the codes of min(max_keep, max_pages * page) tokens of every
+ * sequence, whole pages, since tokens pass through it on their way. */
 int64_t kv_evict_bytes(const km_kv_cache *cache, const km_kv_seqs *seqs, int32_t max_keep);
 
 /* Thread-local message for the last non-OK status ("" if none). */

@@ -388,7 +388,7 @@ def kv_weigh(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, lse: torch.Tensor, w
     q, scale, causal and window are those of the kv_attend call that left lse (its log-sum-exp, float32 [rows, q_heads]).  The call's own
     tokens begin with this sum; with decay = 0 all tokens do.  Rows whose lse is not finite add nothing.  Sequences without rows in the
     call age like the others: their weights are multiplied by decay, with decay = 0 cleared.  No two sequences of a call
-    may have a page in common."""
+    may have a page in common, and none may have one twice."""
     _same(cache, seqs)
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [rows, q_heads, d]")
@@ -413,13 +413,15 @@ def kv_weigh(cache: KvCache, seqs: KvSeqs, q: torch.Tensor, lse: torch.Tensor, w
 def kv_evict(cache: KvCache, seqs: KvSeqs, weight: torch.Tensor, keep: torch.Tensor, max_keep: int, first: int = 0,
              recent: int = 0):
     """Every sequence keeps keep[b] (int32 [n], at most max_keep) of its tokens, each head its own: the first `first`, the last
-    `recent`, then those of the largest weight, ties to the lower position.  They move to the front of the sequence's pages in their
+    `recent`, then those of the largest weight, ties to the lower position.  A keep[b] below first + recent is no error, and then it is
+    the most recent ones that go: give each sequence at least that much.  They move to the front of the sequence's pages in their
     order, with their codes, scales and weights: (kept, lens).
 
     kept: int32 [n, heads, max_keep], the position that each kept token had (-1: none); lens: int32 [n], the sequences' new lengths,
     which the program takes over (``seqs.lens.copy_(lens)``); the pages behind them are free.  Only table and lens of seqs are
     looked at.  Tokens that come later have positions that are no longer their places in the cache: rotary positions are then given
-    to kv_rotate as such.  No two sequences of a call may have a page in common."""
+    to kv_rotate as such.  No two sequences of a call may have a page in common, and none may have one twice.  The workspace is about
+    as large as the codes of the tokens that are kept."""
     _same(cache, seqs)
     _weights(weight, cache)
     _dev(keep, torch.int32, "keep", 1)
