@@ -3,8 +3,8 @@
 // kv_select_kernel, a workgroup for each sequence and head: the K-th largest weight is found digit by digit (11, 11 and
 // 10 bits of the weights' ordered bit patterns, a histogram in LDS for each), then one pass in the order of positions writes down
 // who stays: all above it, and of those equal to it the first.  Few long sequences take several workgroups to a head and a kernel
-// for each of these passes (kv_select_slice_kernel).  kv_gather_kernel, a workgroup for each page that tokens come to, keys or
-// values: builds the page's new contents in the workspace.  kv_scatter_kernel writes them over the page.  In place at once
+// for each of these passes (kv_select_slice_kernel).  kv_gather_kernel, a workgroup for each page that tokens come to:
+// builds the page's new contents in the workspace.  kv_scatter_kernel writes them over the page.  In place at once
 // a page could be written before another has taken its tokens from it: page t takes from pages t and later.  A page whose tokens
 // all stay where they are is left out of both.
 //
@@ -397,95 +397,109 @@ __device__ __forceinline__ bool evict_tile(const EvictArgs &P, EvictTile *o) {
   return true;
 }
 
-// Keys and values by workgroups of their own: one for both, with the loads that lead to a token's page asked for side by side, was 2 %
-// faster where every page changes and 15 % slower in the example below.
+// Keys and values by one workgroup: what takes its time is the chain of loads to a token's page (with one for each, and asked for
+// one after the other, 69.5 us instead of 68.0 in the example below).
 template <int FMT>
 __global__ __launch_bounds__(kGather) void kv_gather_kernel(EvictArgs P) {
   __shared__ int64_t from[128];  // page's head of each slot's token
   __shared__ int tok[128];
-  __shared__ float was[128];
-  __shared__ float top[kGather / 64];
+  __shared__ float was[2][128];  // keys, values
+  __shared__ float top[2][2];
   __shared__ int lpage[128];  // page of the sequence of each slot's token
   __shared__ int64_t pages[128];
   __shared__ __align__(16) uint8_t stage[kStage];
   const KvCache &C = P.C;
-  EvictTile T;
-  if (!evict_tile(P, &T)) return;
+  uint32_t x = P.block0 + blockIdx.x;
+  const int h = (int)(x % (uint32_t)C.heads);
+  x /= (uint32_t)C.heads;
+  const int tile = (int)(x % (uint32_t)P.tiles), b = (int)(x / (uint32_t)P.tiles);
   const int t = threadIdx.x, page = C.page, d = C.d;
-  const int *kept = P.E.kept + T.bh * P.E.max_keep + ((int64_t)T.tile << C.shift);
-  const int *table = P.S.table + (int64_t)T.b * P.S.table_ld;
-  const float *scale = T.values ? C.vs : C.ks;
-  const int64_t slot = T.bh * P.tiles + T.tile;
-  float s = 0.0f;  // the largest scale of this wave's slots
+  const int *table = P.S.table + (int64_t)b * P.S.table_ld;
+  const int64_t bh = (int64_t)b * C.heads + h, slot = bh * P.tiles + tile;
+  // what does not depend on each other is asked for at once, before it is known whether the page changes
+  const int64_t at_kept = ((int64_t)tile << C.shift) + t;
+  const int pos_or = t < page && at_kept < P.E.max_keep ? P.E.kept[bh * P.E.max_keep + at_kept] : -1;
+  const int own_page = table[tile], left = P.E.lens[b];
+  if (!P.moved[slot]) return;  // else the sequence fits, and its pages are there
+  const int n = min(page, left - (tile << C.shift));  // tokens that come to the page
+  float sk = 0.0f, sv = 0.0f;
   if (t < page) {
     // slots behind the last keep their own
-    const bool in = t < T.n;
-    const int pos = in ? kept[t] : 0;
-    const int64_t f = in ? (int64_t)table[pos >> C.shift] * C.heads + T.h : T.to;
+    const bool in = t < n;
+    const int pos = in ? pos_or : 0;
+    const int64_t f = (int64_t)(in ? table[pos >> C.shift] : own_page) * C.heads + h;
     const int k = in ? pos & (page - 1) : t;
     from[t] = f;
     tok[t] = k;
-    lpage[t] = in ? pos >> C.shift : T.tile;
+    lpage[t] = in ? pos >> C.shift : tile;
     if constexpr (FMT == KM_KV_I4) {
-      P.scales[(2 * slot + T.values) * page + t] = scale[f * page + k];
+      P.scales[2 * slot * page + t] = C.ks[f * page + k];
+      P.scales[(2 * slot + 1) * page + t] = C.vs[f * page + k];
     } else {
-      s = scale[f];
-      was[t] = kv_mul_of_scale(s);
-      s = in ? s : 0.0f;
+      sk = C.ks[f];
+      sv = C.vs[f];
+      was[0][t] = kv_mul_of_scale(sk);
+      was[1][t] = kv_mul_of_scale(sv);
+      if (!in) sk = sv = 0.0f;
     }
-    if (!T.values) P.weights[slot * page + t] = P.E.weight[f * page + k];
+    P.weights[slot * page + t] = P.E.weight[f * page + k];
   }
-  float mul = 0.0f;
-  bool again = false;
-  if constexpr (FMT != KM_KV_I4) {
+  float mul[2] = {0.0f, 0.0f};
+  bool again[2] = {false, false};
+  if constexpr (FMT != KM_KV_I4) {  // the largest scales, in the first two waves
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s = fmaxf(s, __shfl_xor(s, o));
-    if ((t & 63) == 0) top[t >> 6] = s;
+    for (int o = 32; o > 0; o >>= 1) {
+      sk = fmaxf(sk, __shfl_xor(sk, o));
+      sv = fmaxf(sv, __shfl_xor(sv, o));
+    }
+    if (t < 128 && (t & 63) == 0) {
+      top[0][t >> 6] = sk;
+      top[1][t >> 6] = sv;
+    }
   }
   __syncthreads();
   if constexpr (FMT != KM_KV_I4) {
-    s = top[0];
-    for (int y = 1; y < kGather / 64; ++y) s = fmaxf(s, top[y]);
-    mul = kv_mul_of_scale(s);
-    if (t == 0) P.scales[2 * slot + T.values] = s;
-    if (t < T.n) again = was[t] > mul;
-    again = __syncthreads_or(again);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float s = fmaxf(top[i][0], top[i][1]);
+      mul[i] = kv_mul_of_scale(s);
+      if (t == i) P.scales[2 * slot + i] = s;
+      again[i] = __syncthreads_or(t < n && was[i][min(t, page - 1)] > mul[i]);
+    }
   }
   const int64_t hb = kv_bytes<FMT>((int64_t)page * d);
   const int db = (int)kv_bytes<FMT>(d);
-  uint8_t *out = P.codes + (2 * slot + T.values) * hb;
+  uint8_t *out = P.codes + 2 * slot * hb;
   // codes whose multiplier was larger, for the page's
-  auto coded = [&](uint32_t w, int i0, int di) {  // codes of slots i0, i0 + di, ...
+  auto coded = [&](int kind, uint32_t w, int i0, int di) {  // codes of slots i0, i0 + di, ...
     if constexpr (FMT != KM_KV_I4) {
       f16x2 lo, hi;
       kv_widen4<FMT>(w, &lo, &hi);
       float x[4] = {(float)lo.x, (float)lo.y, (float)hi.x, (float)hi.y};
 #pragma unroll
-      for (int y = 0; y < 4; ++y) x[y] = x[y] * mul / fmaxf(was[i0 + y * di], mul);
+      for (int y = 0; y < 4; ++y) x[y] = x[y] * mul[kind] / fmaxf(was[kind][i0 + y * di], mul[kind]);
       const uint32_t z = code4<FMT, KM_T_BF16>(x, 1.0f);
       uint32_t keep = 0;  // what lies behind the last slot
 #pragma unroll
-      for (int y = 0; y < 4; ++y) keep |= i0 + y * di < T.n && was[i0 + y * di] > mul ? 0u : 255u << (8 * y);
+      for (int y = 0; y < 4; ++y) keep |= i0 + y * di < n && was[kind][i0 + y * di] > mul[kind] ? 0u : 255u << (8 * y);
       return (w & keep) | (z & ~keep);
     }
     return w;
   };
-  if (!T.values) {
-    const int per = db / 16;
-    for (int i = t; i < page * per; i += kGather) {
-      const int r = i / per, c = i - r * per;
-      u32x4 w = *reinterpret_cast<const u32x4 *>(C.k + from[r] * hb + tok[r] * db + 16 * c);
-      if (again) {
+  const int per = db / 16;
+  for (int i = t; i < page * per; i += kGather) {
+    const int r = i / per, c = i - r * per;
+    u32x4 w = *reinterpret_cast<const u32x4 *>(C.k + from[r] * hb + tok[r] * db + 16 * c);
+    if (again[0]) {
 #pragma unroll
-        for (int y = 0; y < 4; ++y) w[y] = coded(w[y], r, 0);
-      }
-      *reinterpret_cast<u32x4 *>(out + r * db + 16 * c) = w;
+      for (int y = 0; y < 4; ++y) w[y] = coded(0, w[y], r, 0);
     }
-    return;
+    *reinterpret_cast<u32x4 *>(out + r * db + 16 * c) = w;
   }
+  out += hb;
   // Values are taken byte by byte out of rows of `page` bytes.  Where the pages that they come from fit (three of 64 tokens of 128 dims
-  // in 8 bits), those go to LDS in whole lines first: 8 sequences of 4100 tokens, half kept, 56.0 us with their pages read back,
-  // 52.8 so.  Tokens come in the order of positions, so a page's are neighbours: which of the distinct pages is a slot's
+  // in 8 bits), those go to LDS in whole lines first: 8 sequences of 4100 tokens, half kept, 72.8 us with their pages read back,
+  // 69.5 so.  Tokens come in the order of positions, so a page's are neighbours: which of the distinct pages is a slot's
   const int lane = t & 63;
   const bool f0 = lane < page && (lane == 0 || lpage[lane] != lpage[lane - 1]);
   const bool f1 = lane + 64 < page && lpage[lane + 64] != lpage[lane + 63];
@@ -512,9 +526,9 @@ __global__ __launch_bounds__(kGather) void kv_gather_kernel(EvictArgs P) {
       } else {
 #pragma unroll
         for (int y = 0; y < 8; ++y) w[y / 4] |= z[y] << (8 * (y % 4));
-        if (again) {
-          w[0] = coded(w[0], r0, 1);
-          w[1] = coded(w[1], r0 + 4, 1);
+        if (again[1]) {
+          w[0] = coded(1, w[0], r0, 1);
+          w[1] = coded(1, w[1], r0 + 4, 1);
         }
         *reinterpret_cast<u32x2 *>(out + row + r0) = u32x2{w[0], w[1]};
       }
@@ -631,21 +645,21 @@ km_status launch_kv_evict(const KvCache &C, const KvSeqs &S, const KvEvict &E, v
   }
   KMQ_LAUNCH_CHECK("kv_evict");
   const int64_t blocks = kv_evict_blocks(C, S, E.max_keep), most = kv_piece(kGather);
-  auto go = [&](auto *kernel) {
+  auto go = [&](auto *kernel, int64_t blocks) {
     for (int64_t b = 0; b < blocks; b += most) {
       P.block0 = (uint32_t)b;
       kernel<<<dim3((unsigned)std::min(most, blocks - b)), kGather, 0, s>>>(P);
     }
   };
   if (C.fmt == KM_KV_I8) {
-    go(kv_gather_kernel<KM_KV_I8>);
-    go(kv_scatter_kernel<KM_KV_I8>);
+    go(kv_gather_kernel<KM_KV_I8>, blocks / 2);
+    go(kv_scatter_kernel<KM_KV_I8>, blocks);
   } else if (C.fmt == KM_KV_F8) {
-    go(kv_gather_kernel<KM_KV_F8>);
-    go(kv_scatter_kernel<KM_KV_F8>);
+    go(kv_gather_kernel<KM_KV_F8>, blocks / 2);
+    go(kv_scatter_kernel<KM_KV_F8>, blocks);
   } else {
-    go(kv_gather_kernel<KM_KV_I4>);
-    go(kv_scatter_kernel<KM_KV_I4>);
+    go(kv_gather_kernel<KM_KV_I4>, blocks / 2);
+    go(kv_scatter_kernel<KM_KV_I4>, blocks);
   }
   KMQ_LAUNCH_CHECK("kv_evict");
   return KM_OK;
