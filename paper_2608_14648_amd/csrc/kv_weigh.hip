@@ -715,12 +715,14 @@ struct WeighPlan {
 };
 // 32 heads of 128 on 8 unless said otherwise, codes in int8, bf16 rows:
 //   kTokens or kFew: 16 sequences of 500 to 8192 tokens, one row each 19 us and 29, four rows 19 and 29
-//   kFew or kRows: the same, 32 rows each (128 to a cache head) 60 us and 76, 64 rows 102 and 99; 64 of 500 to 4000, 64 rows 172 and 183, 128
-//     rows 310 and 280; two of 3000 to 6000, 64 rows 22 and 25, 1000 rows 235 and 115; 4-bit codes 16 of 500 to 8192, 64 rows
-//     100 and 112.  Heads of 160 and 192 dims leave kRows one wave to a SIMD and kFew two, so that enough positions for all of the
-//     card go through kFew: of 160 dims, 16 of 500 to 8192, 500 rows 521 and 820; two of 3000 to 6000, 192 dims, 3000 rows 817 and 393.
-//   kFew or kShare, fp32: 16 of 500 to 8192, 64 rows 242 us and 374; two of 3000 to 6000, 64 rows 46 and 55, 1000 rows 590 and 362;
-//     one of 2000, 64 rows 31 and 12
+//   kFew or kRows: the same, 32 rows each (128 to a cache head) 60 us and 76, 64 rows 102 and 100; 64 of 500 to 4000, 64 rows 173 and 186, 128
+//     rows 309 and 283; two of 3000 to 6000, 64 rows 21 and 23, 1000 rows 236 and 118; 4-bit codes 16 of 500 to 8192, 64 rows
+//     101 and 110.  From 160 dims on kRows has one wave to a SIMD, and up to 192 kFew two, so that enough positions for all of the
+//     card go through kFew: 16 of 500 to 8192, 500 rows of 160 dims 512 and 803, of 224 879 and 1149, of 256 1178 and 1180, 128 rows of 224 277 and
+//     364, of 256 352 and 385 (4 bits 352 and 401); two of 3000 to 6000, 3000 rows of 192 dims 819 and 384, of 256 967 and 553, but 128 rows of
+//     224 55 and 69.
+//   kFew or kShare, fp32: 16 of 500 to 8192, 64 rows 170 us and 381, 200 rows 471 and 667; two of 3000 to 6000, 64 rows 36 and 56, 250 rows
+//     119 and 118, 1000 rows 454 and 364; one of 2000, 32 rows 15 and 9, 64 rows 25 and 12
 //   workgroups of kTokens, 512, 1024, 2048: 16 of 500 to 8192 22, 19, 19 us; one of 131071 27, 24, 26; 64 of 1 to 16384 (where
 //     1024 are two to a head and 4096 eight) 163, 135, 125, with 4096 122
 //   workgroups of kRows, 512, 1024, 1536, 2048: two prompts of 3133 and 5340 tokens 264, 230, 220, 224 us, without splits 422; pieces of 8
@@ -731,7 +733,7 @@ WeighPlan plan_weigh(const KvCache &C, const KvSeqs &S, const KvAttend &A) {
   const int64_t alone = heads * cdiv(S.max_len, kChunk * kFewWaves);  // workgroups of kFew
   if (rows <= 16) p.way = kTokens;
   else if (A.type == KM_T_F32) p.way = rows >= 1024 || (rows > 64 && alone < 256) ? kShare : kFew;
-  else p.way = rows >= 512 && S.max_rows >= kRowTile && (dim_tiles32(C.d) != 6 || alone < 1024) ? kRows : kFew;
+  else p.way = rows >= 512 && S.max_rows >= kRowTile && (dim_tiles32(C.d) < 6 || alone < 1024) ? kRows : kFew;
   // Workgroups of a sequence's head: one for each of its pieces by the longest length that the caller knows, fewer where that is
   // more than 2^20 in all (a workgroup then takes several, as where a length is longer than was said).
   const int64_t pieces = cdiv(S.max_len, p.way == kShare ? kChunk : p.way == kRows ? kRowKeys : kChunk * kFewWaves);
