@@ -29,8 +29,8 @@
 //
 // 4-bit codes have a scale for each token: the factor ks_j and the logarithm of vs_j are brought to the lane of a position by a
 // broadcast within its sixteen, and widening takes nine instructions for eight codes.  A chunk's codes take half the registers, so
-// four-wave workgroups run three waves to a SIMD: 64 sequences of 1 to 16384 tokens 127 us for 619 MB (two waves, workgroups of eight:
-// 150), one of 131071 of 96 dims in pages of 16 30 us for 118 MB.
+// four-wave workgroups run three waves to a SIMD: 64 sequences of 1 to 16384 tokens 128 us for 619 MB, 4.8 TB/s (two waves, workgroups of eight:
+// 150 us), one of 131071 of 96 dims in pages of 16 30 us for 109 MB.
 #pragma once
 
 #include <type_traits>

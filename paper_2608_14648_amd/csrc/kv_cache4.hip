@@ -10,7 +10,7 @@
 // values holds two tokens, and a page's bytes have one owner, so what the call does not write of a byte is read and kept.
 //
 // Both move 2.5 bytes per 16-bit element and 4 per token and head, and keep the vector unit busy for 60 % of their time: 56691 tokens of 8
-// heads of 128 in bf16 are written in 73 us (295 MB, 4.0 TB/s) and read back in 65 (4.5 TB/s).  Maxima by row operations instead of LDS
+// heads of 128 in bf16 are written in 72 us (295 MB, 4.1 TB/s) and read back in 56 to 63 (4.7 to 5.3 TB/s; cards differ).  Maxima by row operations instead of LDS
 // and codes gathered by byte permutes: 152 -> 143 us for both.
 #include "kv_pages.hpp"
 

@@ -9,9 +9,10 @@
 // all stay where they are is left out of both.
 //
 // Measured: 8 sequences of 4100 tokens, 8 heads of 128 in int8, half of them kept: 12 us to choose (latency: three passes of dependent
-// loads and counts), 35 to gather (a chain of loads to each token's page, values a byte at a time, quotients for codes whose page had another
-// scale), 12 to scatter (34 MB each way, 5.8 TB/s).  One sequence of 100001 tokens, 4-bit codes, 8192 kept: six kernels of 5 to 8 us to
-// choose, each of them mostly its launch and a chain of three dependent loads, 17 to gather, 5 to scatter.
+// loads and counts), 33 to gather (a chain of loads to each token's page, values a byte at a time, quotients for codes whose page had another
+// scale; the vector unit is busy two thirds of the time), 12 to scatter (34 MB each way, 5.5 TB/s).  One sequence of 100001 tokens, 4-bit
+// codes, 8192 kept: six kernels of 4 to 8 us to choose, each of them mostly its launch and a chain of three dependent loads, 13 to gather, 5 to
+// scatter.  The cache is made whole again between calls, here and below.
 #include "kv_pages.hpp"
 
 namespace kmq {
@@ -397,8 +398,9 @@ __device__ __forceinline__ bool evict_tile(const EvictArgs &P, EvictTile *o) {
   return true;
 }
 
-// Keys and values by one workgroup: what takes its time is the chain of loads to a token's page (with one for each, and asked for
-// one after the other, 69.5 us instead of 68.0 in the example below).
+// Keys and values by one workgroup: what takes its time is the chain of loads to a token's page.  With one for each, and asked for one after
+// the other, a call and its read back take 90 us instead of 82 in the example below, 78 instead of 74 for one sequence of 100001 tokens in 4
+// bits.
 template <int FMT>
 __global__ __launch_bounds__(kGather) void kv_gather_kernel(EvictArgs P) {
   __shared__ int64_t from[128];  // page's head of each slot's token
@@ -498,8 +500,10 @@ __global__ __launch_bounds__(kGather) void kv_gather_kernel(EvictArgs P) {
   }
   out += hb;
   // Values are taken byte by byte out of rows of `page` bytes.  Where the pages that they come from fit (three of 64 tokens of 128 dims
-  // in 8 bits), those go to LDS in whole lines first: 8 sequences of 4100 tokens, half kept, 72.8 us with their pages read back,
-  // 69.5 so.  Tokens come in the order of positions, so a page's are neighbours: which of the distinct pages is a slot's
+  // in 8 bits, six in 4; of 128 tokens or 256 dims one and three), those go to LDS in whole lines first.  8 sequences of 4100 tokens, half kept,
+  // their pages read back, with and without that: in 4 bits 61 and 64 us; in int8 82 and 77 (the LDS leaves room for six workgroups instead of
+  // eight), in pages of 16 115 and 96, but where the sequences have been evicted before, so that most pages change little, 61 and 67.
+  // Tokens come in the order of positions, so a page's are neighbours: which of the distinct pages is a slot's
   const int lane = t & 63;
   const bool f0 = lane < page && (lane == 0 || lpage[lane] != lpage[lane - 1]);
   const bool f1 = lane + 64 < page && lpage[lane + 64] != lpage[lane + 63];
@@ -589,10 +593,10 @@ int tiles_of(const KvCache &C, const KvSeqs &S, int max_keep) {
   return (int)std::min<int64_t>(S.max_pages, cdiv(max_keep, C.page));
 }
 
-// Workgroups that choose for a sequence's head: one, but for few long sequences.  One workgroup and slices, 8 heads of 128, 512 tokens
-// kept, us of a whole call: one sequence of 24000 tokens 35 and 42, of 32000 42 and 43, of 40000 47 and 41, of 100001 94 and 45; four of
-// 40000 48 and 56, of 64000 68 and 56; eight of 32000 46 and 60, of 64000 71 and 66; 16 of 64000 82 and 83, of 100001 115 and 111.
-// Slices of 8192 positions instead of 4096: one of 100001 69 instead of 65 with its pages read back.
+// Workgroups that choose for a sequence's head: one, but for few long sequences.  One workgroup and slices, 8 heads of 128 in 4 bits, 512 tokens
+// kept, us of a whole call: one sequence of 24000 tokens 42 and 47, of 32000 48 and 46, of 40000 56 and 49, of 100001 106 and 52; four of
+// 40000 67 and 70, of 64000 89 and 75; eight of 32000 72 and 84, of 64000 102 and 94; 16 of 64000 125 and 129, of 100001 165 and 165.
+// Slices of 8192 positions instead of 4096: one of 100001 54 instead of 52, four of 64000 66 instead of 75.
 int slices_of(const KvCache &C, const KvSeqs &S) {
   const int64_t heads = (int64_t)S.n * C.heads;
   return S.max_len > 32768 + 512 * heads && heads <= 128 ? (int)std::min(cdiv(S.max_len, 4096), 512 / heads) : 1;

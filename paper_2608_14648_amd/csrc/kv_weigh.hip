@@ -15,7 +15,7 @@
 // 500 to 8192 tokens in int8 (13 at the rate of a read; the longest sequence's workgroups are the last).  A few hundred rows:
 // kv_weigh_kernel, each wave with its own positions.  Prompts: kv_weigh_rows_kernel, the waves of a workgroup share tiles of rows in LDS;
 // bound by tiles (a barrier each), the products (matrix cores 25 % busy) and the exponentials (a quarter of the vector unit's rate),
-// which wait for each other: two prompts of 3133 and 5340 tokens, 4-bit codes, 220 to 250 us, 160 GFLOP.  Prompts of fp32 rows:
+// which wait for each other: two prompts of 3133 and 5340 tokens, 4-bit codes, 244 us and 5 to join, 160 GFLOP.  Prompts of fp32 rows:
 // kv_weigh_kernel with a workgroup's waves sharing 64 positions and taking the rows in turn.
 #include "kv_attend.hpp"
 
@@ -40,9 +40,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // bf16 rows: a position's codes are taken times 2^-40, which is exact, or times 1.  f: the softmax's scale in base 2, ks: the position's.
 // |<q, code>| is at most 2^128 448 256 < 2^145.  Where f ks < 1 the sums then stay below 2^105, what products lose below the least normal
-// number is at most 2^-126 256 2^40 = 2^-78 of a score, and a factor that is raised to that number leaves less than 2^-21 of one.  Elsewhere a sum past
+// number changes a score by at most 2^-126 256 2^40 = 2^-78, and a factor that is raised to that number by less than 2^-21.  Elsewhere a sum past
 // 2^128 is a score past 2^128, and the row has no finite log-sum-exp.  4-bit codes: ks lies within [2^-30, 2^30], so f alone decides (f ks < 2^60:
-// the loss is below 2^-18).
+// at most 2^-18).
 template <int FMT, int TYPE>
 __device__ __forceinline__ float weigh_down(float f, float ks) {
   if constexpr (TYPE != KM_T_BF16) return 1.0f;
