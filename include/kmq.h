@@ -499,7 +499,7 @@ km_status kv_read(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_
  *   pool.  Codes of positions inside a sequence have to be finite and their pages' scales finite and not below 2^-100,
  *   I4: their scales within [2^-30, 2^30] (kv_write makes no others); what lies behind its end is not looked at.
  *   fp32 queries: products and weights in two halves each (about 22 bits); 16-bit ones: their own bits, weights rounded to
- *   fp16; sums, maxima and normalisation in fp32.
+ *   fp16 (small ones to within 2^-33 of the row's largest, each times its value's scale); sums, maxima and normalisation in fp32.
  *   The result does not depend on scheduling.
  */
 km_status kv_attend(const km_kv_cache *cache, const km_kv_seqs *seqs, const km_kv_rows *q, int32_t q_heads, float scale,

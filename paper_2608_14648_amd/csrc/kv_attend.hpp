@@ -808,6 +808,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv_join_kernel(AttendArgs P, 
 // reads, 3.3 ms); eight waves to a workgroup (halves the widening, no change).  Heads of more than 128 dims leave a SIMD
 // one wave only, and its phases in turn: 390 TFLOP/s at 256 (pages below 64 also spill up to 10 registers there).
 
+// Weights begin at 2^kUp32 and may grow by kSlack.  Those below fp16's normal range are rounded to whole multiples of 2^-24, so to within 2^-33 of
+// their row's largest, each times its value's scale (with kUp: 2^-40): all that a dim has where the row's heavy tokens have code 0 in it.
 constexpr float kUp32 = 8.0f, kSlack = 7.0f;
 
 typedef float f32x16v __attribute__((ext_vector_type(16)));

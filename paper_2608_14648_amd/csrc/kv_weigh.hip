@@ -41,8 +41,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // bf16 rows: a position's codes are taken times 2^-40, which is exact, or times 1.  f: the softmax's scale in base 2, ks: the position's.
 // |<q, code>| is at most 2^128 448 256 < 2^145.  Where f ks < 1 the sums then stay below 2^105, what products lose below the least normal
 // number changes a score by at most 2^-126 256 2^40 = 2^-78, and a factor that is raised to that number by less than 2^-21.  Elsewhere a sum past
-// 2^128 is a score past 2^128, and the row has no finite log-sum-exp.  4-bit codes: ks lies within [2^-30, 2^30], so f alone decides (f ks < 2^60:
-// at most 2^-18).
+// 2^128 is a score past 2^128, with which the row has no finite log-sum-exp, or past -2^128, which has no weight.  4-bit codes: ks lies within
+// [2^-30, 2^30], so f alone decides (f ks < 2^60: at most 2^-18).
 template <int FMT, int TYPE>
 __device__ __forceinline__ float weigh_down(float f, float ks) {
   if constexpr (TYPE != KM_T_BF16) return 1.0f;
